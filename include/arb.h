@@ -18,7 +18,9 @@
  * Around them: arb_kv_append (the cache write of a step's new tokens), arb_decode_step (one decode token:
  * cache write, attention and length update in one launch), arb_policy (the escalation rules
  * the paper compares on PRM scores: RSD, oracle threshold / arg max, budgeted oracle, with the wasted
- * target calls) and arb_route_classes (the C-way heads of the router ablation).
+ * target calls) and arb_route_classes (the C-way heads of the router ablation).  What a token of a model needs before, inside
+ * and behind the attention: arb_rope_append (norm and rotation of queries and keys with the cache write), arb_attn_rules
+ * (attention with capped, biased and masked scores) and arb_logits (penalties, biases and masks on logits, the next token).
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless the argument says "host".  The caller owns every tensor;
@@ -492,6 +494,149 @@ arb_status arb_kv_append_i4(arb_ctx *ctx, const arb_attn_params *params, int32_t
                             const void *v_new, const int32_t *block_table, int32_t *seq_lens, const int32_t *new_lens,
                             int32_t update_lens, uint8_t *k_codes, uint8_t *v_codes, float *k_scales, float *v_scales,
                             arb_stream_t stream);
+
+/*
+ * ---- Before the attention: norm, rotation and cache write in one pass -----------------------------
+ * The paper's Algorithm 1 samples steps from models whose forward passes it does not describe; arb_attn takes queries and
+ * keys whose position rotation has been applied.  These calls take a projection's raw rows instead: queries and keys are
+ * normed per head (where weights are given), rotated, and the keys go into the paged cache with the values, as
+ * arb_kv_append would write them.
+ *
+ * For every (token, head) row x of D values of a query or a key, in fp32:
+ *   norm      y = x * rsqrt(mean(x^2) + eps) * weight      (a NULL weight: y = x)
+ *   rotation  angle_p = pos * inv_freq[p], p < rot_dim / 2; the pair (a, b) number p becomes
+ *             (a cos - b sin, a sin + b cos).  interleaved == 0: pair p is (p, p + rot_dim / 2); else (2p, 2p + 1).
+ *             Dimensions from rot_dim on pass through.  The angle is reduced in 64 bits, so far positions lose nothing.
+ * rounded once, to the type of the output.  Values are written as they are.
+ */
+typedef struct {
+    int32_t rot_dim;          /* 0 (no rotation) .. head_dim, a multiple of 16 */
+    int32_t interleaved;      /* how dimensions pair up, see above */
+    float eps;                /* >= 0 */
+    int32_t reserved;         /* 0 */
+    int64_t q_stride;         /* elements from a token's first query row to the next token's; 0: num_q_heads * head_dim. */
+    int64_t k_stride;         /* Likewise of k_new and v_new (0: num_kv_heads * head_dim).  A projection that leaves queries, */
+    int64_t v_stride;         /* keys and values side by side passes three pointers and one stride.  Multiples of 16 bytes. */
+    const float *q_weight;    /* fp32 [head_dim], nullable; 16-byte aligned, as are the next two */
+    const float *k_weight;    /* fp32 [head_dim], nullable */
+    const float *inv_freq;    /* fp32 [rot_dim / 2], finite; may be NULL when rot_dim is 0 */
+    const int32_t *positions; /* int32 [total_new], nullable: the positions that rotate; NULL: the rows' places in the cache */
+} arb_rope_params;
+
+/*
+ *   params     dtype (of q, k_new, v_new, q_out and the pools), batch, num_q_heads, num_kv_heads, head_dim (64 or 128),
+ *              page_size, num_pages and max_pages_per_seq are used; num_q_heads need not be a multiple of num_kv_heads.
+ *   q          [total_new, Hq, D], k_new, v_new [total_new, Hkv, D], rows packed by sequence in batch order, tokens
+ *              rope->*_stride elements apart.
+ *   seq_lens, new_lens, update_lens, block_table
+ *              as for arb_kv_append: token j of sequence b goes to position seq_lens[b] + j.
+ *   q_out      [total_new, Hq, D], dense; may be q itself where q is dense.  Rows beyond the sum of new_lens are left alone.
+ * A sequence that arb_kv_append would refuse is refused here too, with the same status bit: its pools and length stay as they
+ * are and its rows of q_out are zero-filled.
+ * Errors: ARB_ERR_INVALID_ARG, ARB_ERR_UNSUPPORTED (dtype, head_dim, page size, batch, rot_dim, more than 2^31 - 1 rows
+ * of all heads), ARB_ERR_CUDA.
+ */
+arb_status arb_rope_append(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope, int32_t total_new,
+                           const void *q, const void *k_new, const void *v_new, const int32_t *block_table,
+                           int32_t *seq_lens, const int32_t *new_lens, int32_t update_lens, void *q_out, void *k_pages,
+                           void *v_pages, arb_stream_t stream);
+
+/* arb_rope_append into an E4M3 cache: code = e4m3(y * inv_scale) of the normed and rotated key in fp32 (one rounding), of the
+ * value as it is; everything else of the format as for arb_kv_append_e4m3. */
+arb_status arb_rope_append_e4m3(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope,
+                                int32_t total_new, const void *q, const void *k_new, const void *v_new,
+                                float k_inv_scale, float v_inv_scale, const int32_t *block_table, int32_t *seq_lens,
+                                const int32_t *new_lens, int32_t update_lens, void *q_out, uint8_t *k_codes,
+                                uint8_t *v_codes, arb_stream_t stream);
+
+/* arb_rope_append into the 4-bit cache of arb_decode_step_i4: dtype ARB_BF16, head_dim 128; scale and codes are taken from
+ * the normed and rotated key in fp32.  k_codes, v_codes uint8 [num_pages, Hkv, P, D / 2], k_scales, v_scales fp32
+ * [num_pages, Hkv, P]. */
+arb_status arb_rope_append_i4(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope, int32_t total_new,
+                              const void *q, const void *k_new, const void *v_new, const int32_t *block_table,
+                              int32_t *seq_lens, const int32_t *new_lens, int32_t update_lens, void *q_out,
+                              uint8_t *k_codes, uint8_t *v_codes, float *k_scales, float *v_scales, arb_stream_t stream);
+
+/*
+ * ---- Inside the attention: rules on the scores ---------------------------------------------------
+ * arb_attn for models whose scores are not the plain scaled product (the paper's attention is the models' own, of which it
+ * says nothing).  With s = softmax_scale * q . k_j of a query token at position pos and query head h:
+ *   cap > 0         s <- cap * tanh(s / cap)
+ *   slopes          s <- s - slopes[h] * |pos - j|
+ *   what a token sees is a range of keys j:
+ *     from          max(0, first_keys[row], pos - window + 1)     (first_keys, window: where given)
+ *     to            pos; or prefix_lens[b] - 1 for a token that lies inside its sequence's prefix (pos < prefix_lens[b]),
+ *                   which reads the prefix both ways.  A prefix beyond seq_lens[b] counts as seq_lens[b].
+ * A token that sees no key gets a row of zeros.
+ */
+typedef struct {
+    float cap;                   /* 0: scores are not capped */
+    int32_t window;              /* keys a token sees up to itself, itself included; 0: no window */
+    const float *slopes;         /* fp32 [num_q_heads], nullable, finite */
+    const int32_t *prefix_lens;  /* int32 [B], nullable; <= 0: no prefix */
+    const int32_t *first_keys;   /* int32 [total_q], nullable: first key of the document a token belongs to */
+} arb_score_rules;
+
+/*
+ * Arguments, layouts, status bits and asynchrony as for arb_attn (q_lens 0, 1 or a step length; bf16 or fp32); with every
+ * rule off the result is arb_attn's, within its tolerance.  Keys that no token of a sequence sees do not reach the result,
+ * whatever they hold; where a step has tokens that see a key and tokens that do not, its value has to be finite (its key row
+ * may hold anything).
+ * Block-table entries of pages without a visible key are not read.
+ * params->flags must be 0.
+ * Errors: ARB_ERR_INVALID_ARG (cap or window negative, cap not finite), ARB_ERR_UNSUPPORTED (flags, and what arb_attn
+ * does not support), ARB_ERR_WORKSPACE, ARB_ERR_CUDA.
+ */
+arb_status arb_attn_rules(arb_ctx *ctx, const arb_attn_params *params, const arb_score_rules *rules, const void *q,
+                          const void *k_pages, const void *v_pages, const int32_t *block_table, const int32_t *seq_lens,
+                          const int32_t *q_lens, void *out, arb_stream_t stream);
+
+/*
+ * ---- Behind the attention: from logits to the next token -------------------------------------------
+ * Section 3.1 samples a step token by token, z_i ~ q(z_i | x, z_<i); the models' logits and what requests ask of them are not
+ * the paper's subject.  For every row s and token t, in fp32, each operation rounded once (IEEE):
+ *   x = logits[s][t]
+ *   c = times t occurs in history[s][0 .. history_lens[s]);  where c > 0:
+ *       x = x > 0 ? x / repetition[s] : x * repetition[s];   x = x - presence[s];   x = x - frequency[s] * c
+ *   x = x + (sum of bias_values of t in row s, in the order of the list)
+ *   x = x / temperature[s] where temperature[s] > 0
+ *   x = -inf where bit t % 32 of mask[s][t / 32] is 0
+ * and, per row:
+ *   tokens[s]    the lowest t whose x + noise[s][t] is largest (noise that is Gumbel-distributed makes this a draw from
+ *                softmax(x)); a row with temperature[s] <= 0 ignores its noise.  NaN never wins; -1 if every x is -inf or NaN.
+ *   logprobs[s]  x[tokens[s]] - log sum_t exp(x[t])   (NaN where a NaN or +inf is among x; -inf where the token is -1)
+ * Every pointer of this record but logits may be NULL: the step is left out, the output is not wanted.
+ */
+typedef struct {
+    int32_t dtype;                /* of logits: ARB_F32 or ARB_BF16 */
+    int32_t rows, vocab;
+    int32_t history_stride;       /* tokens from one row of history to the next */
+    int64_t logits_stride;        /* elements from one row of logits to the next; 0: vocab */
+    const void *logits;           /* [rows, vocab] */
+    const int32_t *history;       /* int32 [rows, history_stride]; tokens outside 0 .. vocab - 1 count for nothing */
+    const int32_t *history_lens;  /* int32 [rows], clamped to 0 .. history_stride; NULL: history_stride */
+    const float *repetition, *presence, *frequency;   /* fp32 [rows] each; without history they do nothing */
+    const int32_t *bias_offsets;  /* int32 [rows + 1], not decreasing: row s has entries bias_offsets[s] .. [s + 1] - 1 */
+    const int32_t *bias_tokens;   /* tokens outside 0 .. vocab - 1 count for nothing */
+    const float *bias_values;
+    int32_t bias_total;           /* entries of bias_tokens and bias_values; offsets are clamped to 0 .. bias_total */
+    int32_t mask_stride;          /* 32-bit words from one row of mask to the next, >= ceil(vocab / 32) */
+    const uint32_t *mask;         /* 1 = allowed */
+    const float *temperature;     /* fp32 [rows] */
+    const float *noise;           /* fp32 [rows, vocab], dense */
+    float *out;                   /* fp32 [rows, vocab], dense: x; may be logits itself where those are fp32 and dense */
+    int32_t *tokens;              /* int32 [rows] */
+    float *logprobs;              /* fp32 [rows] */
+} arb_logits_params;
+
+/*
+ * One pass over the logits: every slice of a row is adjusted, written and reduced by one CTA; the CTA of a row that finishes
+ * last puts the slices' maxima and sums together, always in the same order.  Uses the ctx's arrival counters and step
+ * workspace.
+ * Errors: ARB_ERR_INVALID_ARG (no logits, nothing wanted, bad sizes or strides, bias or history incomplete),
+ * ARB_ERR_UNSUPPORTED (dtype, more than 65535 rows, vocab above 2^24), ARB_ERR_WORKSPACE, ARB_ERR_CUDA.
+ */
+arb_status arb_logits(arb_ctx *ctx, const arb_logits_params *params, arb_stream_t stream);
 
 /*
  * Spearman's rank correlation of two samples (Section 4.2, "Evaluation", and Tables 1-3 of the paper:

@@ -47,6 +47,7 @@ EXPORTS = ("arb_create", "arb_destroy", "arb_attn_workspace_bytes", "arb_attn", 
            "arb_attn_host_begin", "arb_attn_host_wait",
            "arb_attn_decode_static", "arb_decode_step", "arb_decode_step_e4m3", "arb_decode_step_i4", "arb_kv_append_i4",
            "arb_route", "arb_rollback", "arb_policy", "arb_route_classes", "arb_kv_append", "arb_kv_append_e4m3", "arb_attn_decode_e4m3", "arb_attn_e4m3", "arb_phase_lens", "arb_phase_lens_tokens", "arb_spearman",
+           "arb_rope_append", "arb_rope_append_e4m3", "arb_rope_append_i4", "arb_attn_rules", "arb_logits",
            "arb_selftest_wait_timeout", "arb_selftest_guard_zones", "arb_poll_status", "arb_launch_count", "arb_status_string")
 
 
@@ -56,6 +57,27 @@ class AttnParams(ctypes.Structure):
                 ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
                 ("total_q", ctypes.c_int32), ("max_q_len", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("flags", ctypes.c_uint32)]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
+class ScoreRules(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("prefix_lens", ctypes.c_void_p), ("first_keys", ctypes.c_void_p)]
+
+
+class LogitsParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "rows", "vocab", "history_stride")]
+                + [("logits_stride", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("logits", "history", "history_lens", "repetition", "presence",
+                                                  "frequency", "bias_offsets", "bias_tokens", "bias_values")]
+                + [("bias_total", ctypes.c_int32), ("mask_stride", ctypes.c_int32)]
+                + [(n, ctypes.c_void_p) for n in ("mask", "temperature", "noise", "out", "tokens", "logprobs")])
 
 
 _vp, _i32, _f = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
@@ -108,6 +130,17 @@ lib.arb_route_classes.argtypes = [_vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, c
                                   _vp, _vp, _vp, _vp]
 lib.arb_kv_append.restype = ctypes.c_int
 lib.arb_kv_append.argtypes = [_vp, ctypes.POINTER(AttnParams), _i32, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
+lib.arb_rope_append.restype = ctypes.c_int
+lib.arb_rope_append.argtypes = [_vp, ctypes.POINTER(AttnParams), ctypes.POINTER(RopeParams), _i32] + [_vp] * 6 + [_i32] + [_vp] * 4
+lib.arb_rope_append_e4m3.restype = ctypes.c_int
+lib.arb_rope_append_e4m3.argtypes = ([_vp, ctypes.POINTER(AttnParams), ctypes.POINTER(RopeParams), _i32] + [_vp] * 3 + [_f, _f]
+                                     + [_vp] * 3 + [_i32] + [_vp] * 4)
+lib.arb_rope_append_i4.restype = ctypes.c_int
+lib.arb_rope_append_i4.argtypes = [_vp, ctypes.POINTER(AttnParams), ctypes.POINTER(RopeParams), _i32] + [_vp] * 6 + [_i32] + [_vp] * 6
+lib.arb_attn_rules.restype = ctypes.c_int
+lib.arb_attn_rules.argtypes = [_vp, ctypes.POINTER(AttnParams), ctypes.POINTER(ScoreRules)] + [_vp] * 8
+lib.arb_logits.restype = ctypes.c_int
+lib.arb_logits.argtypes = [_vp, ctypes.POINTER(LogitsParams), _vp]
 lib.arb_selftest_wait_timeout.restype = ctypes.c_int
 lib.arb_selftest_wait_timeout.argtypes = [_vp, ctypes.c_int64, _vp, _vp]
 lib.arb_selftest_guard_zones.restype = ctypes.c_int
@@ -185,6 +218,8 @@ def attn_decode_static(q, k_pages, v_pages, block_table, seq_lens, q_lens, out=N
 class Context:
     """Owns one arb_ctx on a CUDA device (split-KV workspace, status word, staging buffers)."""
 
+    _device = 0   # index of that device
+
     def __init__(self, device=0, workspace_bytes: int = 0):
         self.device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
         torch.cuda.init()
@@ -193,6 +228,7 @@ class Context:
             _check(lib.arb_create(ctypes.byref(h), self.device.index or 0, workspace_bytes), "arb_create")
         self._h = h
         self._p = int(h.value)   # the handle as the extension module takes it
+        self._device = self.device.index or 0
 
     def close(self):
         if getattr(self, "_h", None):
@@ -365,6 +401,76 @@ class Context:
         if st:
             _check(st, "arb_kv_append_e4m3")
         return seq_lens
+
+    # -- arb_rope_append ----------------------------------------------------------------------
+    def rope_append(self, q, k_new, v_new, inv_freq, block_table, seq_lens, new_lens, k_pages, v_pages, q_weight=None,
+                    k_weight=None, eps: float = 1e-6, interleaved: bool = False, positions=None, q_out=None,
+                    update_lens: bool = True, stream=None):
+        """Norm (where weights are given), rotation and cache write in one pass: returns q_out [total, Hq, D], the
+        normed and rotated queries; the keys, treated alike, and the values go behind each sequence's tokens.  q, k_new and
+        v_new may be views of one projection (dense per token, any stride between tokens that is a multiple of 16 bytes);
+        inv_freq fp32 [rot_dim / 2], weights fp32 [D].  Asynchronous."""
+        return self._rope(0, q, k_new, v_new, inv_freq, 1.0, 1.0, block_table, seq_lens, new_lens, k_pages, v_pages, None, None,
+                          q_weight, k_weight, eps, interleaved, positions, q_out, update_lens, stream)
+
+    def rope_append_e4m3(self, q, k_new, v_new, inv_freq, k_inv_scale: float, v_inv_scale: float, block_table, seq_lens,
+                         new_lens, k_codes, v_codes, q_weight=None, k_weight=None, eps: float = 1e-6,
+                         interleaved: bool = False, positions=None, q_out=None, update_lens: bool = True, stream=None):
+        """rope_append into an E4M3 cache (code = e4m3(x * inv_scale))."""
+        return self._rope(1, q, k_new, v_new, inv_freq, k_inv_scale, v_inv_scale, block_table, seq_lens, new_lens, k_codes,
+                          v_codes, None, None, q_weight, k_weight, eps, interleaved, positions, q_out, update_lens, stream)
+
+    def rope_append_i4(self, q, k_new, v_new, inv_freq, block_table, seq_lens, new_lens, k_codes, v_codes, k_scales, v_scales,
+                       q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, positions=None,
+                       q_out=None, update_lens: bool = True, stream=None):
+        """rope_append into a 4-bit cache (codes uint8 [pages, Hkv, P, D / 2], scales fp32 [pages, Hkv, P])."""
+        return self._rope(2, q, k_new, v_new, inv_freq, 1.0, 1.0, block_table, seq_lens, new_lens, k_codes, v_codes, k_scales,
+                          v_scales, q_weight, k_weight, eps, interleaved, positions, q_out, update_lens, stream)
+
+    def _rope(self, form, q, k_new, v_new, inv_freq, k_inv, v_inv, block_table, seq_lens, new_lens, k_pool, v_pool, k_scales,
+              v_scales, q_weight, k_weight, eps, interleaved, positions, q_out, update_lens, stream):
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        st = _native.rope_append(self._p, self._device, form, q, k_new, v_new, inv_freq, k_inv, v_inv, block_table, seq_lens,
+                                 new_lens, k_pool, v_pool, k_scales, v_scales, q_weight, k_weight, eps, interleaved, positions,
+                                 q_out, update_lens, stream)
+        if st:
+            _check(st, ("arb_rope_append", "arb_rope_append_e4m3", "arb_rope_append_i4")[form])
+        return q_out
+
+    # -- arb_attn_rules -----------------------------------------------------------------------
+    def attn_rules(self, q, k_pages, v_pages, block_table, seq_lens, q_lens, max_q_len: int, cap: float = 0.0, window: int = 0,
+                   slopes=None, prefix_lens=None, first_keys=None, out=None, softmax_scale: float = 0.0, stream=None):
+        """attn for models with rules on the scores: cap * tanh(s / cap), a bias -slopes[h] * distance, a window of keys, a
+        prefix that is read both ways, the first key of each token's document.  Asynchronous."""
+        if out is None:
+            out = torch.empty_like(q)
+        st = _native.attn_rules(self._p, self._device, q, k_pages, v_pages, block_table, seq_lens, q_lens, max_q_len, cap, window,
+                                slopes, prefix_lens, first_keys, out, softmax_scale, stream)
+        if st:
+            _check(st, "arb_attn_rules")
+        return out
+
+    # -- arb_logits ---------------------------------------------------------------------------
+    def logits(self, logits, history=None, history_lens=None, repetition=None, presence=None, frequency=None,
+               bias_offsets=None, bias_tokens=None, bias_values=None, mask=None, temperature=None, noise=None, out=None,
+               tokens=None, logprobs=None, want_out: bool = True, stream=None):
+        """Penalties, biases, temperature and allowed-token mask on logits [S, V] (fp32 or bf16, contiguous rows), and the next
+        token: returns (out fp32 [S, V], tokens int32 [S], logprobs fp32 [S]); out is None with want_out=False.
+        Per-request arrays are fp32 [S]; history int32 [S, H]; the biases of row s are entries bias_offsets[s] ..
+        bias_offsets[s + 1] - 1 of bias_tokens / bias_values; mask int32 words [S, >= ceil(V / 32)].  Asynchronous."""
+        S = logits.shape[0]
+        if out is None and want_out:
+            out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+        if tokens is None:
+            tokens = torch.empty(S, dtype=torch.int32, device=logits.device)
+        if logprobs is None:
+            logprobs = torch.empty(S, dtype=torch.float32, device=logits.device)
+        st = _native.logits(self._p, self._device, logits, history, history_lens, repetition, presence, frequency, bias_offsets,
+                            bias_tokens, bias_values, mask, temperature, noise, out, tokens, logprobs, stream)
+        if st:
+            _check(st, "arb_logits")
+        return out, tokens, logprobs
 
     # -- arb_spearman -------------------------------------------------------------------------
     def spearman(self, x, y, rho=None, stream=None):

@@ -135,6 +135,49 @@ void pipe_teardown(Ctx *c) {
     if (c->out_stream) cudaStreamDestroy(c->out_stream);
 }
 
+// What the three forms of arb_rope_append check alike; nothing to do when total_new is 0.
+arb_status check_rope(const arb_attn_params *p, const arb_rope_params *rope, int32_t total_new, const void *q, const void *k_new,
+                      const void *v_new, const int32_t *block_table, const int32_t *seq_lens, const int32_t *new_lens,
+                      const void *q_out, const void *k_pool, const void *v_pool) {
+    if (p == nullptr || rope == nullptr || total_new < 0) return ARB_ERR_INVALID_ARG;
+    if (p->batch < 1 || p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_pages < 1 || p->max_pages_per_seq < 1)
+        return ARB_ERR_INVALID_ARG;
+    if (p->dtype != ARB_F32 && p->dtype != ARB_BF16) return ARB_ERR_UNSUPPORTED;
+    if (p->head_dim != 64 && p->head_dim != 128) return ARB_ERR_UNSUPPORTED;
+    if (p->page_size != kPage || p->batch > kMaxBatch) return ARB_ERR_UNSUPPORTED;
+    if ((long long)p->max_pages_per_seq * kPage > (1ll << 30)) return ARB_ERR_UNSUPPORTED;
+    if (rope->reserved != 0 || rope->rot_dim < 0 || !(rope->eps >= 0.f)) return ARB_ERR_INVALID_ARG;
+    if (rope->rot_dim > p->head_dim || rope->rot_dim % 16 != 0) return ARB_ERR_UNSUPPORTED;
+    if (rope->rot_dim > 0 && !rope->inv_freq) return ARB_ERR_INVALID_ARG;
+    if (!aligned16(rope->q_weight) || !aligned16(rope->k_weight) || !aligned16(rope->inv_freq)) return ARB_ERR_INVALID_ARG;
+    const int64_t per16 = p->dtype == ARB_BF16 ? 8 : 4, q_row = (int64_t)p->num_q_heads * p->head_dim,
+                  kv_row = (int64_t)p->num_kv_heads * p->head_dim;
+    if ((rope->q_stride != 0 && rope->q_stride < q_row) || (rope->k_stride != 0 && rope->k_stride < kv_row) ||
+        (rope->v_stride != 0 && rope->v_stride < kv_row) || rope->q_stride % per16 || rope->k_stride % per16 || rope->v_stride % per16)
+        return ARB_ERR_INVALID_ARG;
+    if (!block_table || !seq_lens || !new_lens || !k_pool || !v_pool) return ARB_ERR_INVALID_ARG;
+    if (total_new == 0) return ARB_OK;
+    if (total_new * ((long long)p->num_q_heads + 2ll * p->num_kv_heads) > INT32_MAX) return ARB_ERR_UNSUPPORTED;
+    if (!q || !k_new || !v_new || !q_out) return ARB_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(k_pool) || !aligned16(v_pool))
+        return ARB_ERR_INVALID_ARG;
+    return ARB_OK;
+}
+
+arb_status rope_append(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope, int32_t total_new, const void *q,
+                       const void *k_new, const void *v_new, RopeCache cache, float ki, float vi, const int32_t *block_table,
+                       int32_t *seq_lens, const int32_t *new_lens, int32_t update_lens, void *q_out, void *k_pool, void *v_pool,
+                       float *k_scales, float *v_scales, arb_stream_t stream) {
+    if (ctx == nullptr) return ARB_ERR_INVALID_ARG;
+    const arb_status st = check_rope(params, rope, total_new, q, k_new, v_new, block_table, seq_lens, new_lens, q_out, k_pool, v_pool);
+    if (st != ARB_OK || total_new == 0) return st;
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return ARB_ERR_CUDA;
+    return launch_rope_append(c, *params, *rope, total_new, q, k_new, v_new, cache, ki, vi, block_table, seq_lens, new_lens,
+                              update_lens, q_out, k_pool, v_pool, k_scales, v_scales, reinterpret_cast<cudaStream_t>(stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -739,6 +782,79 @@ arb_status arb_kv_append_i4(arb_ctx *ctx, const arb_attn_params *params, int32_t
     return launch_kv_append_i4(reinterpret_cast<Ctx *>(ctx), *params, total_new, k_new, v_new, block_table, seq_lens,
                                new_lens, update_lens, k_codes, v_codes, k_scales, v_scales,
                                reinterpret_cast<cudaStream_t>(stream));
+}
+
+arb_status arb_rope_append(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope, int32_t total_new,
+                           const void *q, const void *k_new, const void *v_new, const int32_t *block_table,
+                           int32_t *seq_lens, const int32_t *new_lens, int32_t update_lens, void *q_out, void *k_pages,
+                           void *v_pages, arb_stream_t stream) {
+    return rope_append(ctx, params, rope, total_new, q, k_new, v_new, RopeCache::kSame, 1.f, 1.f, block_table, seq_lens, new_lens,
+                       update_lens, q_out, k_pages, v_pages, nullptr, nullptr, stream);
+}
+
+arb_status arb_rope_append_e4m3(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope,
+                                int32_t total_new, const void *q, const void *k_new, const void *v_new,
+                                float k_inv_scale, float v_inv_scale, const int32_t *block_table, int32_t *seq_lens,
+                                const int32_t *new_lens, int32_t update_lens, void *q_out, uint8_t *k_codes,
+                                uint8_t *v_codes, arb_stream_t stream) {
+    if (!(k_inv_scale > 0.f) || !(v_inv_scale > 0.f)) return ARB_ERR_INVALID_ARG;
+    return rope_append(ctx, params, rope, total_new, q, k_new, v_new, RopeCache::kE4m3, k_inv_scale, v_inv_scale, block_table,
+                       seq_lens, new_lens, update_lens, q_out, k_codes, v_codes, nullptr, nullptr, stream);
+}
+
+arb_status arb_rope_append_i4(arb_ctx *ctx, const arb_attn_params *params, const arb_rope_params *rope, int32_t total_new,
+                              const void *q, const void *k_new, const void *v_new, const int32_t *block_table,
+                              int32_t *seq_lens, const int32_t *new_lens, int32_t update_lens, void *q_out,
+                              uint8_t *k_codes, uint8_t *v_codes, float *k_scales, float *v_scales, arb_stream_t stream) {
+    if (params == nullptr) return ARB_ERR_INVALID_ARG;
+    if (params->dtype != ARB_BF16 || params->head_dim != 128) return ARB_ERR_UNSUPPORTED;
+    if (!k_scales || !v_scales || !aligned16(k_scales) || !aligned16(v_scales)) return ARB_ERR_INVALID_ARG;
+    return rope_append(ctx, params, rope, total_new, q, k_new, v_new, RopeCache::kI4, 1.f, 1.f, block_table, seq_lens, new_lens,
+                       update_lens, q_out, k_codes, v_codes, k_scales, v_scales, stream);
+}
+
+arb_status arb_attn_rules(arb_ctx *ctx, const arb_attn_params *params, const arb_score_rules *rules, const void *q,
+                          const void *k_pages, const void *v_pages, const int32_t *block_table, const int32_t *seq_lens,
+                          const int32_t *q_lens, void *out, arb_stream_t stream) {
+    if (ctx == nullptr || rules == nullptr) return ARB_ERR_INVALID_ARG;
+    const arb_status st = check_params(params);
+    if (st != ARB_OK) return st;
+    if (params->flags != 0) return ARB_ERR_UNSUPPORTED;
+    if (!(rules->cap >= 0.f) || rules->cap > 3.0e38f || rules->window < 0) return ARB_ERR_INVALID_ARG;
+    if (!k_pages || !v_pages || !block_table || !seq_lens || !q_lens) return ARB_ERR_INVALID_ARG;
+    if (params->total_q == 0 || params->max_q_len == 0) return ARB_OK;  // nothing to do
+    if (!q || !out) return ARB_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(k_pages) || !aligned16(v_pages)) return ARB_ERR_INVALID_ARG;
+    if (params->max_q_len > params->total_q) return ARB_ERR_INVALID_ARG;
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    if (decode_workspace_bytes(*params, c->num_sms) > c->workspace_bytes) return ARB_ERR_WORKSPACE;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return ARB_ERR_CUDA;
+    return launch_attn_rules(c, *params, *rules, q, k_pages, v_pages, block_table, seq_lens, q_lens, out,
+                             reinterpret_cast<cudaStream_t>(stream));
+}
+
+arb_status arb_logits(arb_ctx *ctx, const arb_logits_params *params, arb_stream_t stream) {
+    if (ctx == nullptr || params == nullptr) return ARB_ERR_INVALID_ARG;
+    const arb_logits_params &p = *params;
+    if (p.dtype != ARB_F32 && p.dtype != ARB_BF16) return ARB_ERR_UNSUPPORTED;
+    if (p.rows < 0 || p.vocab < 1 || (p.logits_stride != 0 && p.logits_stride < p.vocab)) return ARB_ERR_INVALID_ARG;
+    if (p.rows > 65535 || p.vocab > (1 << 24)) return ARB_ERR_UNSUPPORTED;
+    if (p.history ? p.history_stride < 1 : p.history_lens != nullptr) return ARB_ERR_INVALID_ARG;
+    if (p.bias_offsets ? (p.bias_total < 0 || (p.bias_total > 0 && (!p.bias_tokens || !p.bias_values)))
+                       : (p.bias_tokens || p.bias_values))
+        return ARB_ERR_INVALID_ARG;
+    if (p.mask && (long long)p.mask_stride * 32 < p.vocab) return ARB_ERR_INVALID_ARG;
+    if (!p.out && !p.tokens && !p.logprobs) return ARB_ERR_INVALID_ARG;
+    if (p.rows == 0) return ARB_OK;
+    if (!p.logits) return ARB_ERR_INVALID_ARG;
+    const size_t elt = p.dtype == ARB_BF16 ? 2 : 4;
+    auto misaligned = [](const void *q, size_t n) { return (reinterpret_cast<uintptr_t>(q) & (n - 1)) != 0; };
+    if (misaligned(p.logits, elt) || misaligned(p.noise, 4) || misaligned(p.out, 4)) return ARB_ERR_INVALID_ARG;
+    Ctx *c = reinterpret_cast<Ctx *>(ctx);
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return ARB_ERR_CUDA;
+    return launch_logits(c, p, reinterpret_cast<cudaStream_t>(stream));
 }
 
 arb_status arb_poll_status(arb_ctx *ctx, arb_stream_t stream, uint32_t *bits) {

@@ -26,7 +26,7 @@ struct Raised {};   // a Python error is set
     X(arb_attn) X(arb_attn_host) X(arb_attn_host_begin) X(arb_attn_host_wait) X(arb_decode_step) X(arb_decode_step_e4m3)  \
     X(arb_decode_step_i4) X(arb_kv_append) X(arb_kv_append_e4m3) X(arb_kv_append_i4) X(arb_attn_decode_e4m3)               \
     X(arb_attn_e4m3) X(arb_route) X(arb_rollback) X(arb_policy) X(arb_route_classes) X(arb_spearman) X(arb_phase_lens)     \
-    X(arb_phase_lens_tokens)
+    X(arb_phase_lens_tokens) X(arb_rope_append) X(arb_rope_append_e4m3) X(arb_rope_append_i4) X(arb_attn_rules) X(arb_logits)
 
 struct Library {
 #define X(f) decltype(&::f) f = nullptr;
@@ -449,6 +449,190 @@ METHOD(spearman) {
     });
 }
 
+// Tensors of the calls below live on the context's device, which the Python side passes as a number.
+void *on(const at::Tensor &t, const char *name, int device) {
+    void *p = dev(t, name);
+    if ((int)t.get_device() != device) fail(PyExc_ValueError, "%s must be on the context's device", name);
+    return p;
+}
+void *on(const at::Tensor &t, const char *name, int device, at::ScalarType want) {
+    void *p = dev(t, name, want);
+    if ((int)t.get_device() != device) fail(PyExc_ValueError, "%s must be on the context's device", name);
+    return p;
+}
+void *on(PyObject *o, const char *name, int device, at::ScalarType want) { return on(tensor(o, name), name, device, want); }
+void *on_or_null(PyObject *o, const char *name, int device, at::ScalarType want) {
+    return o == Py_None ? nullptr : on(o, name, device, want);
+}
+// ... of `count` elements
+void *sized(const at::Tensor &t, const char *name, int device, at::ScalarType want, int64_t count) {
+    if (t.numel() != count) {
+        PyErr_Format(PyExc_ValueError, "%s must have %lld elements, got %lld", name, (long long)count, (long long)t.numel());
+        throw Raised();
+    }
+    return on(t, name, device, want);
+}
+void *sized(PyObject *o, const char *name, int device, at::ScalarType want, int64_t count) {
+    return sized(tensor(o, name), name, device, want, count);
+}
+void *sized_or_null(PyObject *o, const char *name, int device, at::ScalarType want, int64_t count) {
+    return o == Py_None ? nullptr : sized(o, name, device, want, count);
+}
+// None: the device's current stream
+arb_stream_t stream_on(PyObject *o, int device) {
+    return o == Py_None ? (arb_stream_t)at::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream() : stream_of(o);
+}
+void same_shape(const at::Tensor &t, const at::Tensor &as, const char *name, const char *other) {
+    if (t.sizes() != as.sizes()) fail(PyExc_ValueError, "%s must have the shape of %s", name, other);
+}
+
+// Rows [tokens, heads, D] of a projection: a token's heads are dense, tokens may be any multiple of 16 bytes apart.
+struct Rows {
+    void *p;
+    int64_t stride;   // elements between tokens, 0: dense
+};
+void rows_shaped(const at::Tensor &t, const char *name, int64_t tokens, int64_t heads, int64_t dim) {
+    if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != heads || t.size(2) != dim) {
+        PyErr_Format(PyExc_ValueError, "%s has to be [%lld, %lld, %lld]", name, (long long)tokens, (long long)heads, (long long)dim);
+        throw Raised();
+    }
+}
+Rows rows_of(const at::Tensor &t, const char *name, int device, at::ScalarType want) {
+    const int64_t tokens = t.size(0), heads = t.size(1), dim = t.size(2);
+    if (!t.is_cuda() || (tokens > 0 && (t.stride(2) != 1 || (heads > 1 && t.stride(1) != dim) || (tokens > 1 && t.stride(0) < heads * dim))))
+        fail(PyExc_ValueError, "%s must be a CUDA tensor whose tokens' rows are contiguous", name);
+    if ((int)t.get_device() != device) fail(PyExc_ValueError, "%s must be on the context's device", name);
+    if (t.scalar_type() != want) fail(PyExc_TypeError, "%s must be torch.%s, got torch.%s", name, dtype_name(want), dtype_name(t.scalar_type()));
+    return {t.data_ptr(), tokens > 1 ? t.stride(0) : 0};
+}
+
+// (h, device, form, q, k_new, v_new, inv_freq, k_inv_scale, v_inv_scale, block_table, seq_lens, new_lens, k_pool, v_pool, k_scales,
+//  v_scales, q_weight, k_weight, eps, interleaved, positions, q_out, update_lens, stream); form 0: pools of q's type, 1: E4M3, 2: 4-bit
+METHOD(rope_append) {
+    return guarded(n, 24, [&] {
+        const int device = integer(a[1]), form = integer(a[2]);
+        const at::Tensor &q = of_rank(tensor(a[3], "q"), 3, "q"), &kn = of_rank(tensor(a[4], "k_new"), 3, "k_new");
+        const at::Tensor &bt = of_rank(tensor(a[9], "block_table"), 2, "block_table");
+        const at::Tensor &kp = of_rank(tensor(a[12], "the pool"), 4, "the pool"), &vp = of_rank(tensor(a[13], "the pool"), 4, "the pool");
+        const auto dt = q.scalar_type(), pool_type = form == 0 ? dt : kU8;
+        const int64_t T = q.size(0), hq = q.size(1), D = q.size(2), hkv = kn.size(1), B = bt.size(0);
+        arb_attn_params p = {dtype_code(q), (int)B, (int)hq, (int)hkv, (int)D, (int)kp.size(2), (int)kp.size(0), (int)bt.size(1), (int)T, 0, 0.0f, 0u};
+        if (kp.size(1) != hkv || kp.size(3) != (form == 2 ? D / 2 : D)) fail(PyExc_ValueError, "%s", "the pools do not match k_new");
+        same_shape(vp, kp, "v's pool", "k's");
+        if (T > INT32_MAX) fail(PyExc_ValueError, "%s", "too many tokens");
+        const at::Tensor &vn = tensor(a[5], "v_new"), &freq = tensor(a[6], "inv_freq");
+        rows_shaped(kn, "k_new", T, hkv, D);
+        rows_shaped(vn, "v_new", T, hkv, D);
+        arb_rope_params r = {};
+        if (freq.numel() > D / 2) fail(PyExc_ValueError, "%s", "inv_freq has more than head_dim / 2 elements");
+        const Rows qr = rows_of(q, "q", device, dt), kr = rows_of(kn, "k_new", device, dt), vr = rows_of(vn, "v_new", device, dt);
+        r.rot_dim = 2 * (int)freq.numel();
+        r.inv_freq = F32(on(freq, "inv_freq", device, at::kFloat));
+        r.q_weight = F32(sized_or_null(a[16], "q_weight", device, at::kFloat, D));
+        r.k_weight = F32(sized_or_null(a[17], "k_weight", device, at::kFloat, D));
+        r.eps = to_float(a[18]);
+        r.interleaved = PyObject_IsTrue(a[19]);
+        r.positions = I32(sized_or_null(a[20], "positions", device, kI32, T));
+        r.q_stride = qr.stride; r.k_stride = kr.stride; r.v_stride = vr.stride;
+        const float ki = to_float(a[7]), vi = to_float(a[8]);
+        void *t = on(bt, "block_table", device, kI32), *sl = sized(a[10], "seq_lens", device, kI32, B), *nl = sized(a[11], "new_lens", device, kI32, B);
+        void *k = on(kp, "k's pool", device, pool_type), *v = on(vp, "v's pool", device, pool_type);
+        void *ks = nullptr, *vs = nullptr;
+        if (form == 2) {
+            ks = sized(a[14], "k_scales", device, at::kFloat, kp.size(0) * hkv * kp.size(2));
+            vs = sized(a[15], "v_scales", device, at::kFloat, kp.size(0) * hkv * kp.size(2));
+        }
+        void *qo = sized(a[21], "q_out", device, dt, T * hq * D);
+        const int update = PyObject_IsTrue(a[22]);
+        arb_ctx *h = context(a[0]);
+        arb_stream_t s = stream_on(a[23], device);
+        return without_gil([&] {
+            if (form == 1) return lib.arb_rope_append_e4m3(h, &p, &r, (int)T, qr.p, kr.p, vr.p, ki, vi, I32(t), I32(sl), I32(nl), update, qo, U8(k), U8(v), s);
+            if (form == 2) return lib.arb_rope_append_i4(h, &p, &r, (int)T, qr.p, kr.p, vr.p, I32(t), I32(sl), I32(nl), update, qo, U8(k), U8(v), F32(ks), F32(vs), s);
+            return lib.arb_rope_append(h, &p, &r, (int)T, qr.p, kr.p, vr.p, I32(t), I32(sl), I32(nl), update, qo, k, v, s);
+        });
+    });
+}
+
+// (h, device, q, k_pages, v_pages, block_table, seq_lens, q_lens, max_q_len, cap, window, slopes, prefix_lens, first_keys, out, softmax_scale, stream)
+METHOD(attn_rules) {
+    return guarded(n, 17, [&] {
+        const int device = integer(a[1]);
+        const at::Tensor &q = tensor(a[2], "q"), &kp = tensor(a[3], "k_pages"), &vp = tensor(a[4], "v_pages"), &bt = tensor(a[5], "block_table");
+        const arb_attn_params p = params_for(q, kp, bt, integer(a[8]), a[15], 0, Py_None);
+        same_shape(vp, kp, "v_pages", "k_pages");
+        if (kp.size(3) != q.size(2)) fail(PyExc_ValueError, "%s", "k_pages and q have different head dimensions");
+        const auto dt = q.scalar_type();
+        arb_score_rules r = {};
+        r.cap = to_float(a[9]);
+        r.window = integer(a[10]);
+        void *qp = on(q, "q", device, dt), *k = on(kp, "k_pages", device, dt), *v = on(vp, "v_pages", device, dt);
+        void *t = on(bt, "block_table", device, kI32), *sl = sized(a[6], "seq_lens", device, kI32, p.batch), *ql = sized(a[7], "q_lens", device, kI32, p.batch);
+        r.slopes = F32(sized_or_null(a[11], "slopes", device, at::kFloat, p.num_q_heads));
+        r.prefix_lens = I32(sized_or_null(a[12], "prefix_lens", device, kI32, p.batch));
+        r.first_keys = I32(sized_or_null(a[13], "first_keys", device, kI32, p.total_q));
+        void *out = sized(a[14], "out", device, dt, q.numel());
+        arb_ctx *h = context(a[0]);
+        arb_stream_t s = stream_on(a[16], device);
+        return without_gil([&] { return lib.arb_attn_rules(h, &p, &r, qp, k, v, I32(t), I32(sl), I32(ql), out, s); });
+    });
+}
+
+// (h, device, logits, history, history_lens, repetition, presence, frequency, bias_offsets, bias_tokens, bias_values, mask, temperature,
+//  noise, out, tokens, logprobs, stream)
+METHOD(logits) {
+    return guarded(n, 18, [&] {
+        const int device = integer(a[1]);
+        const at::Tensor &x = of_rank(tensor(a[2], "logits"), 2, "logits");
+        arb_logits_params p = {};
+        p.dtype = dtype_code(x);
+        const int64_t S = x.size(0), V = x.size(1);
+        if (S > INT32_MAX || V > INT32_MAX) fail(PyExc_ValueError, "%s", "logits are too large");
+        p.rows = (int)S;
+        p.vocab = (int)V;
+        if (!x.is_cuda() || (V > 1 && x.stride(1) != 1) || (S > 1 && x.stride(0) < V)) fail(PyExc_ValueError, "%s", "logits must be a CUDA tensor of contiguous rows");
+        if ((int)x.get_device() != device) fail(PyExc_ValueError, "%s must be on the context's device", "logits");
+        p.logits = x.data_ptr();
+        p.logits_stride = S > 1 ? x.stride(0) : 0;
+        if (a[3] != Py_None) {
+            const at::Tensor &hist = of_rank(tensor(a[3], "history"), 2, "history");
+            if (hist.size(1) > 0) {
+                p.history = I32(sized(hist, "history", device, kI32, S * hist.size(1)));
+                p.history_stride = (int)hist.size(1);
+                p.history_lens = I32(sized_or_null(a[4], "history_lens", device, kI32, S));
+            }
+        } else if (a[4] != Py_None) {
+            fail(PyExc_ValueError, "%s", "history_lens without history");
+        }
+        p.repetition = F32(sized_or_null(a[5], "repetition", device, at::kFloat, S));
+        p.presence = F32(sized_or_null(a[6], "presence", device, at::kFloat, S));
+        p.frequency = F32(sized_or_null(a[7], "frequency", device, at::kFloat, S));
+        if ((a[8] == Py_None) != (a[9] == Py_None) || (a[8] == Py_None) != (a[10] == Py_None))
+            fail(PyExc_ValueError, "%s", "bias_offsets, bias_tokens and bias_values go together");
+        if (a[8] != Py_None) {
+            const at::Tensor &tokens = tensor(a[9], "bias_tokens");
+            p.bias_offsets = I32(sized(a[8], "bias_offsets", device, kI32, S + 1));
+            p.bias_tokens = I32(on(tokens, "bias_tokens", device, kI32));
+            p.bias_values = F32(sized(a[10], "bias_values", device, at::kFloat, tokens.numel()));
+            p.bias_total = (int)tokens.numel();
+        }
+        if (a[11] != Py_None) {
+            const at::Tensor &mask = of_rank(tensor(a[11], "mask"), 2, "mask");
+            if (mask.size(1) * 32 < V) fail(PyExc_ValueError, "%s", "mask has too few words for the vocabulary");
+            p.mask = static_cast<uint32_t *>(sized(mask, "mask", device, kI32, S * mask.size(1)));
+            p.mask_stride = (int)mask.size(1);
+        }
+        p.temperature = F32(sized_or_null(a[12], "temperature", device, at::kFloat, S));
+        p.noise = F32(sized_or_null(a[13], "noise", device, at::kFloat, S * V));
+        p.out = F32(sized_or_null(a[14], "out", device, at::kFloat, S * V));
+        p.tokens = I32(sized_or_null(a[15], "tokens", device, kI32, S));
+        p.logprobs = F32(sized_or_null(a[16], "logprobs", device, at::kFloat, S));
+        arb_ctx *h = context(a[0]);
+        arb_stream_t s = stream_on(a[17], device);
+        return without_gil([&] { return lib.arb_logits(h, &p, s); });
+    });
+}
+
 // (handle of the opened library): looks its functions up
 PyObject *bind(PyObject *, PyObject *handle) {
     void *h = PyLong_AsVoidPtr(handle);
@@ -475,6 +659,7 @@ PyMethodDef methods[] = {
     ENTRY(attn), ENTRY(attn_host), ENTRY(attn_host_wait), ENTRY(decode_step), ENTRY(decode_step_e4m3), ENTRY(decode_step_i4),
     ENTRY(kv_append), ENTRY(kv_append_e4m3), ENTRY(kv_append_i4), ENTRY(attn_e4m3), ENTRY(route), ENTRY(route_classes),
     ENTRY(rollback), ENTRY(phase_lens), ENTRY(phase_lens_tokens), ENTRY(policy), ENTRY(spearman),
+    ENTRY(rope_append), ENTRY(attn_rules), ENTRY(logits),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -570,7 +570,7 @@ arb_status arb_rope_append_i4(arb_ctx *ctx, const arb_attn_params *params, const
  * A token that sees no key gets a row of zeros.
  */
 typedef struct {
-    float cap;                   /* 0: scores are not capped */
+    float cap;                   /* 1e-20 .. 1e20; 0: scores are not capped */
     int32_t window;              /* keys a token sees up to itself, itself included; 0: no window */
     const float *slopes;         /* fp32 [num_q_heads], nullable, finite */
     const int32_t *prefix_lens;  /* int32 [B], nullable; <= 0: no prefix */
@@ -579,12 +579,12 @@ typedef struct {
 
 /*
  * Arguments, layouts, status bits and asynchrony as for arb_attn (q_lens 0, 1 or a step length; bf16 or fp32); with every
- * rule off the result is arb_attn's, within its tolerance.  Keys that no token of a sequence sees do not reach the result,
- * whatever they hold; where a step has tokens that see a key and tokens that do not, its value has to be finite (its key row
- * may hold anything).
+ * rule off the result is arb_attn's, within its tolerance.  Keys before the first and behind the last key that any of a
+ * sequence's tokens sees do not reach the result, whatever they hold; of the keys between the two the values have to be
+ * finite (the key rows of hidden ones may hold anything).
  * Block-table entries of pages without a visible key are not read.
  * params->flags must be 0.
- * Errors: ARB_ERR_INVALID_ARG (cap or window negative, cap not finite), ARB_ERR_UNSUPPORTED (flags, and what arb_attn
+ * Errors: ARB_ERR_INVALID_ARG (cap outside its range, window negative), ARB_ERR_UNSUPPORTED (flags, and what arb_attn
  * does not support), ARB_ERR_WORKSPACE, ARB_ERR_CUDA.
  */
 arb_status arb_attn_rules(arb_ctx *ctx, const arb_attn_params *params, const arb_score_rules *rules, const void *q,

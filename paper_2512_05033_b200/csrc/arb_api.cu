@@ -820,7 +820,7 @@ arb_status arb_attn_rules(arb_ctx *ctx, const arb_attn_params *params, const arb
     const arb_status st = check_params(params);
     if (st != ARB_OK) return st;
     if (params->flags != 0) return ARB_ERR_UNSUPPORTED;
-    if (!(rules->cap >= 0.f) || rules->cap > 3.0e38f || rules->window < 0) return ARB_ERR_INVALID_ARG;
+    if (!(rules->cap == 0.f || (rules->cap >= 1e-20f && rules->cap <= 1e20f)) || rules->window < 0) return ARB_ERR_INVALID_ARG;
     if (!k_pages || !v_pages || !block_table || !seq_lens || !q_lens) return ARB_ERR_INVALID_ARG;
     if (params->total_q == 0 || params->max_q_len == 0) return ARB_OK;  // nothing to do
     if (!q || !out) return ARB_ERR_INVALID_ARG;

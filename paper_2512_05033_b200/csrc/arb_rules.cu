@@ -1,4 +1,5 @@
-// Attention with rules on the scores (arb_attn_rules): a warp per (query row, head), keys in groups of 32.
+// Attention with rules on the scores (arb_attn_rules): bf16 on the tensor-core chunk kernel; fp32 here, a warp per (query row,
+// head), keys in groups of 32.
 #include "arb_rules.cuh"
 
 namespace arb {
@@ -105,14 +106,12 @@ arb_status launch_attn_rules(Ctx *ctx, const arb_attn_params &p, const arb_score
     a.scale_log2 = a.scale * 1.4426950408889634f;
     a.rules = {rules.cap > 0.f ? a.scale / rules.cap : 0.f, rules.cap * 1.4426950408889634f, rules.window, rules.slopes,
                rules.prefix_lens, rules.first_keys};
+    if (p.dtype == ARB_BF16)
+        return launch_chunk_rules(ctx, p, a.rules, 1, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
     const dim3 grid(ctx->num_sms * 8);
     const size_t smem = sizeof(int) * ((size_t)p.batch + 1);
-    cudaError_t err;
-    if (p.dtype == ARB_BF16)
-        err = p.head_dim == 128 ? launch_pdl(rules_kernel<__nv_bfloat16, 128>, grid, dim3(kThreads), smem, stream, a)
-                                : launch_pdl(rules_kernel<__nv_bfloat16, 64>, grid, dim3(kThreads), smem, stream, a);
-    else
-        err = p.head_dim == 128 ? launch_pdl(rules_kernel<float, 128>, grid, dim3(kThreads), smem, stream, a)
+    const cudaError_t err =
+        p.head_dim == 128 ? launch_pdl(rules_kernel<float, 128>, grid, dim3(kThreads), smem, stream, a)
                                 : launch_pdl(rules_kernel<float, 64>, grid, dim3(kThreads), smem, stream, a);
     ctx->launches++;
     return err == cudaSuccess ? ARB_OK : ARB_ERR_CUDA;

@@ -141,7 +141,6 @@ struct MmaArgs {
 
 struct RuledArgs : MmaArgs {
     Rules rules;
-    int min_q_len;      // 1: decode rows are served here too
 };
 template <bool RULED>
 using ArgsOf = std::conditional_t<RULED, RuledArgs, MmaArgs>;
@@ -381,13 +380,9 @@ __device__ __forceinline__ Plan plan_arrays(int *base, int B) {
     return pl;
 }
 
-__device__ __forceinline__ int min_q_len(const MmaArgs &) { return 2; }
-__device__ __forceinline__ int min_q_len(const RuledArgs &a) { return a.min_q_len; }
-
 // A chunk whose lengths fit: what this kernel serves.  One whose lengths do not has its rows zero-filled.
-template <class Args>
-__device__ __forceinline__ bool chunk_ok(const Args &a, int n, int L) {
-    return n >= min_q_len(a) && n <= a.rows && L >= n && L <= a.max_pages * kPage;
+__device__ __forceinline__ bool chunk_ok(const MmaArgs &a, int n, int L) {
+    return n >= 2 && n <= a.rows && L >= n && L <= a.max_pages * kPage;
 }
 
 // Query rows (tokens times heads of the group) of a sequence that q and out have: all of them, unless the q_lens on the
@@ -707,7 +702,7 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
     make_plan<G>(a, pl, tid, threads_of(E4M3));
     for (int b = blockIdx.x; b < B; b += gridDim.x) {
         const int n = a.q_lens[b];
-        if (n < min_q_len(a) || pl.pairs[b] > 0) continue;
+        if (n < 2 || pl.pairs[b] > 0) continue;
         if (tid == 0) atomicOr(a.status, (uint32_t)ARB_DEV_BAD_SEQ_LEN);
         const int there = rows_there<1>(a, pl.row0[b], n);
         for (int i = pl.row0[b]; i < pl.row0[b] + there; ++i) {

@@ -14,7 +14,7 @@ arb_status launch_g(Ctx *ctx, const RuledArgs &a, int head_dim, const CUtensorMa
 
 }  // namespace
 
-arb_status launch_chunk_rules(Ctx *ctx, const arb_attn_params &p, const Rules &rules, int min_q_len, const void *q, const void *k_pages,
+arb_status launch_chunk_rules(Ctx *ctx, const arb_attn_params &p, const Rules &rules, const void *q, const void *k_pages,
                               const void *v_pages, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens,
                               void *out, cudaStream_t stream) {
     alignas(64) CUtensorMap km, vm;
@@ -25,7 +25,6 @@ arb_status launch_chunk_rules(Ctx *ctx, const arb_attn_params &p, const Rules &r
     RuledArgs a;
     fill_args(a, ctx, p, q, k_pages, v_pages, 1.0f, 1.0f, block_table, seq_lens, q_lens, out, false);
     a.rules = rules;
-    a.min_q_len = min_q_len;
     const int g = p.num_q_heads / p.num_kv_heads, max_items = most_items(a, p);
     switch (g) {
         case 1: return launch_g<1>(ctx, a, p.head_dim, km, vm, max_items, stream);

@@ -1,15 +1,26 @@
 // From logits to the next token (arb_logits, see arb.h for the formulas): penalties for tokens a row's history holds, biases,
 // temperature, an allowed-token mask, the arg max of x + noise and its log-probability.
 //
-// One pass over memory: a row of logits is cut into slices of kSlice tokens and a CTA takes one slice.  It asks for its logits
-// and noise first, then counts the history's tokens that fall into the slice (integer atomics in shared memory: any order
-// gives the same counts) and adds up the biases (one warp walks the list in order, so that a token listed twice gets its sum
-// in the order of the list), and only then adjusts, writes and reduces what it holds in registers.  A history is read by every
-// CTA of its row, from L2.  The slices' maxima and sums go to the workspace; the CTA of a row that arrives last at the row's
-// counter puts them together, slice by slice in order.
+// One pass over memory: a row is cut into pieces of kPiece tokens, and its pieces into as many runs as keep every resident CTA
+// busy, one CTA a run.  Few tokens of a vocabulary are in a history or a list of biases, so these are gone through on their own:
+// the CTA counts the history's tokens that fall into a piece (integer atomics in shared memory: any order gives the same
+// counts), lists every token that occurs there or among the biases once, and gives the listed ones their penalties and
+// biases (each bias added by any thread, unless a token is listed twice: then its first entry's thread sums them up in the
+// order of the list).  The stream over the piece, which does temperature, mask, noise, maximum and sum, takes a listed token's
+// value, which a bit per token marks, from shared memory.  A history is read by every CTA of its row, from L2.  The runs' records
+// (maximum, sum, best) go to the workspace; the CTA of a row that arrives last at the row's counter puts them together, run by
+// run in order.
 //
-// Rows of an odd vocabulary start at any element, so a thread's eight tokens are cut at multiples of eight of the flat element
+// What bounds it is instruction issue, the barriers around the special tokens and what a CTA waits for at its end.  64 rows of
+// 128001 bf16 logits (49 MB; a plain bf16 -> fp32 copy of them takes 24 us): 16 us without options, 47 us with a history of up to 4096
+// tokens, biases, mask, temperature and noise (84 MB).  Looking up a count and a bias for every token 53 us; a CTA per piece instead
+// of a run of pieces 19 and 56 us (every CTA's reduction, fence and arrival cost 7 us); the special tokens in a kernel of their own
+// 20 and 61 us.
+//
+// Rows of an odd vocabulary start at any element, so groups of four tokens are cut at multiples of four of the flat element
 // index: full groups are aligned in every array whose rows lie alike, a row's first and last group are read one by one.
+#include <type_traits>
+
 #include "arb_common.cuh"
 
 namespace arb {
@@ -17,11 +28,13 @@ namespace arb {
 namespace {
 
 constexpr int kLogitsThreads = 256;
-constexpr int kGroup = 8;                                   // tokens of a vector load
-constexpr int kPerThread = 2;                               // groups of a thread
-constexpr int kSlice = kLogitsThreads * kPerThread * kGroup;
+constexpr int kLogitsCtas = 4;                              // resident CTAs of an SM
+constexpr int kGroup = 4;                                   // tokens of a vector load
+template <int PER> constexpr int kPiece = kLogitsThreads * PER * kGroup;   // PER groups a thread
+constexpr int kHeld = 8;                                    // history tokens of a thread in flight
+constexpr int kBiasOne = 1 << 24;                           // in a token's counter: history below, entries of the biases above
 
-struct Record {      // what a slice leaves: max and sum of exponentials of x, the best x + noise with its token and its x
+struct Record {      // what a run leaves of a row: max and sum of exponentials of x, the best x + noise with its token and its x
     float m, l, best, best_x;
     int token;
     int pad[3];
@@ -29,10 +42,17 @@ struct Record {      // what a slice leaves: max and sum of exponentials of x, t
 
 struct LogitsArgs {
     arb_logits_params p;
-    Record *records;
+    Record *records;     // [rows][runs]
     int *counters;
-    int slices;      // most that a row has
+    int pieces;          // of a row
 };
+
+// asks [from, from + bytes) into L2, but for the ends that share a 16-byte piece with something else
+__device__ __forceinline__ void prefetch_l2(const void *from, long long bytes) {
+    const uintptr_t begin = (reinterpret_cast<uintptr_t>(from) + 15) & ~uintptr_t(15), end = (reinterpret_cast<uintptr_t>(from) + bytes) & ~uintptr_t(15);
+    if (bytes > 0 && end > begin)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(begin), "r"((uint32_t)(end - begin)) : "memory");
+}
 
 // the better of two candidates: larger, then lower token; token < 0: none
 __device__ __forceinline__ bool beats(float a, int ta, float b, int tb) {
@@ -46,199 +66,382 @@ __device__ __forceinline__ void merge(Record &a, const Record &o) {
     if (beats(o.best, o.token, a.best, a.token)) { a.best = o.best; a.best_x = o.best_x; a.token = o.token; }
 }
 
-__device__ __forceinline__ Record shfl_xor(const Record &r, int off) {
-    Record o;
-    o.m = __shfl_xor_sync(0xffffffffu, r.m, off);
-    o.l = __shfl_xor_sync(0xffffffffu, r.l, off);
-    o.best = __shfl_xor_sync(0xffffffffu, r.best, off);
-    o.best_x = __shfl_xor_sync(0xffffffffu, r.best_x, off);
-    o.token = __shfl_xor_sync(0xffffffffu, r.token, off);
-    return o;
+// floats as unsigned integers of the same order; NaN is not among them
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float warp_max(float x) {
+    const uint32_t u = __reduce_max_sync(0xffffffffu, ordered(x));
+    return __uint_as_float(u ^ ((int)u < 0 ? 0x80000000u : 0xffffffffu));
+}
+// best, best_x and token of the warp's best candidate, in every lane
+__device__ __forceinline__ void best_of_warp(Record &r) {
+    const float best = warp_max(r.token < 0 ? -INFINITY : r.best + 0.0f);   // (-0 and 0 are a tie)
+    const uint32_t token = __reduce_min_sync(0xffffffffu, r.token >= 0 && r.best == best ? (uint32_t)r.token : 0xffffffffu);
+    const uint32_t who = __ballot_sync(0xffffffffu, r.token >= 0 && (uint32_t)r.token == token);
+    r.best_x = __shfl_sync(0xffffffffu, r.best_x, who ? __ffs(who) - 1 : 0);
+    r.best = best;
+    r.token = (int)token;   // -1: nobody had one
+}
+// the records of a warp's lanes into one, in every lane
+__device__ __forceinline__ void merge_warp(Record &r) {
+    const float m = warp_max(r.m), base = m == -INFINITY ? 0.f : m;
+    r.l *= __expf(r.m - base);
+    r.m = m;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) r.l += __shfl_xor_sync(0xffffffffu, r.l, off);
+    best_of_warp(r);
 }
 
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&x)[8]);
-template <>
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
-    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-template <>
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&x)[8]) {
-    Elt<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4 *>(p), x);
-}
+__device__ __forceinline__ void none_yet(Record &r) { r.m = -INFINITY; r.l = 0.f; r.best = -INFINITY; r.best_x = -INFINITY; r.token = -1; }
 
-template <typename T>
-__global__ void __launch_bounds__(kLogitsThreads)
-logits_kernel(const LogitsArgs a) {
-    const arb_logits_params &p = a.p;
-    extern __shared__ int counts[];                       // [kSlice], then the biases [kSlice]; each where the call has any
-    __shared__ Record warp_rec[kLogitsThreads / 32];
-    __shared__ int last;
-    const bool history = p.history != nullptr, biased = p.bias_offsets != nullptr;
-    float *bias = reinterpret_cast<float *>(counts + (history ? kSlice : 0));
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int row = blockIdx.y, V = p.vocab;
-    const long long stride = p.logits_stride ? p.logits_stride : V;
-    const T *x_in = static_cast<const T *>(p.logits) + row * stride;
-    const float *noise = p.noise ? p.noise + (size_t)row * V : nullptr;
-    float *out = p.out ? p.out + (size_t)row * V : nullptr;
-    pdl_enter();
-
-    // groups of eight start where the logits' own alignment has them; the dense fp32 arrays' groups agree or are taken one by one
-    const int skew = (int)((reinterpret_cast<uintptr_t>(x_in) / sizeof(T)) & (kGroup - 1));
-    const bool noise_alike = noise && (int)((reinterpret_cast<uintptr_t>(noise) / 4) & 3) == (skew & 3);
-    const bool out_alike = out && (int)((reinterpret_cast<uintptr_t>(out) / 4) & 3) == (skew & 3);
-    const int lo = (int)blockIdx.x * kSlice - skew;       // first token of the slice (below 0: the row starts inside a group)
-    const float temperature = p.temperature ? p.temperature[row] : 1.0f;
-    const bool noisy = noise && temperature > 0.f;
-
-    float x[kPerThread][kGroup], g[kPerThread][kGroup];
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k) {
-        const int t0 = lo + (k * kLogitsThreads + tid) * kGroup;
-        if (t0 >= 0 && t0 + kGroup <= V) {
-            load8<T>(x_in + t0, x[k]);
-            if (noisy && noise_alike) load8<float>(noise + t0, g[k]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kGroup; ++i) x[k][i] = (t0 + i >= 0 && t0 + i < V) ? Elt<T>::to_float(x_in[t0 + i]) : -INFINITY;
-        }
-        if (noisy && !(noise_alike && t0 >= 0 && t0 + kGroup <= V)) {
-#pragma unroll
-            for (int i = 0; i < kGroup; ++i) g[k][i] = (t0 + i >= 0 && t0 + i < V) ? noise[t0 + i] : 0.f;
-        }
-    }
-
-    if (history || biased) {
-        for (int i = tid; i < kSlice / 4; i += kLogitsThreads) {
-            if (history) reinterpret_cast<int4 *>(counts)[i] = make_int4(0, 0, 0, 0);
-            if (biased) reinterpret_cast<float4 *>(bias)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        __syncthreads();
-        if (history) {
-            const int n = p.history_lens ? max(0, min(p.history_lens[row], p.history_stride)) : p.history_stride;
-            const int32_t *h = p.history + (size_t)row * p.history_stride;
-            for (int i = tid; i < n; i += kLogitsThreads) {
-                const int t = h[i];
-                if (t >= 0 && t < V && (unsigned)(t - lo) < (unsigned)kSlice) atomicAdd(&counts[t - lo], 1);
-            }
-        }
-        if (biased && warp == 0) {
-            const int begin = max(0, min(p.bias_offsets[row], p.bias_total)), end = max(0, min(p.bias_offsets[row + 1], p.bias_total));
-            for (int i0 = begin; i0 < end; i0 += 32) {
-                const int i = i0 + lane;
-                const int t = i < end ? p.bias_tokens[i] : -1;
-                const bool mine = t >= 0 && t < V && (unsigned)(t - lo) < (unsigned)kSlice;
-                const float value = mine ? p.bias_values[i] : 0.f;
-                const int key = mine ? t - lo : -1 - lane;
-                const uint32_t same = __match_any_sync(0xffffffffu, key);
-                if (__any_sync(0xffffffffu, __popc(same) > 1)) {   // a token listed twice: its values one after the other
-                    for (int k = 0; k < 32; ++k) {
-                        if (lane == k && mine) bias[key] = __fadd_rn(bias[key], value);
-                        __syncwarp();
-                    }
-                } else if (mine) {
-                    bias[key] = __fadd_rn(bias[key], value);
-                }
-                __syncwarp();
-            }
-        }
-        __syncthreads();
-    }
-
-    const float repetition = history && p.repetition ? p.repetition[row] : 1.0f;
-    const float presence = history && p.presence ? p.presence[row] : 0.0f;
-    const float frequency = history && p.frequency ? p.frequency[row] : 0.0f;
-    const uint32_t *mask = p.mask ? p.mask + (size_t)row * p.mask_stride : nullptr;
-    Record r;
-    r.m = -INFINITY; r.l = 0.f; r.best = -INFINITY; r.best_x = -INFINITY; r.token = -1;
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k) {
-        const int at = (k * kLogitsThreads + tid) * kGroup, t0 = lo + at;
-        if (t0 >= V) continue;
-        uint32_t allowed = 0xffu;
-        if (mask) {   // bits t0 .. t0 + 7; t0 may lie below 0 and the eight bits in two words
-            const int w = max(t0, 0) >> 5, w_last = (V - 1) >> 5;
-            const unsigned long long bits = (unsigned long long)mask[w] | (unsigned long long)mask[min(w + 1, w_last)] << 32;
-            allowed = t0 >= 0 ? (uint32_t)(bits >> (t0 & 31)) : (uint32_t)bits << -t0;
-        }
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i) {
-            const int t = t0 + i;
-            float v = x[k][i];
-            if (history) {
-                const int c = counts[at + i];
-                if (c > 0) {
-                    v = v > 0.f ? __fdiv_rn(v, repetition) : __fmul_rn(v, repetition);
-                    v = __fsub_rn(v, presence);
-                    v = __fsub_rn(v, __fmul_rn(frequency, (float)c));
-                }
-            }
-            if (biased) v = __fadd_rn(v, bias[at + i]);
-            if (p.temperature && temperature > 0.f) v = __fdiv_rn(v, temperature);
-            const bool real = t >= 0 && t < V;
-            if (!real || !((allowed >> i) & 1u)) v = -INFINITY;
-            x[k][i] = v;
-            const float y = noisy ? __fadd_rn(v, g[k][i]) : v;
-            if (y > r.best) { r.best = y; r.best_x = v; r.token = t; }
-        }
-        if (out) {
-            if (out_alike && t0 >= 0 && t0 + kGroup <= V) {
-                *reinterpret_cast<float4 *>(out + t0) = make_float4(x[k][0], x[k][1], x[k][2], x[k][3]);
-                *reinterpret_cast<float4 *>(out + t0 + 4) = make_float4(x[k][4], x[k][5], x[k][6], x[k][7]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kGroup; ++i)
-                    if (t0 + i >= 0 && t0 + i < V) out[t0 + i] = x[k][i];
-            }
-        }
-    }
-    if (!p.tokens && !p.logprobs) return;
-
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k) {
-        if (lo + (k * kLogitsThreads + tid) * kGroup >= V) continue;
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i) r.m = fmaxf(r.m, x[k][i]);
-    }
-    const float base = r.m == -INFINITY ? 0.f : r.m;
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k) {
-        if (lo + (k * kLogitsThreads + tid) * kGroup >= V) continue;
-#pragma unroll
-        for (int i = 0; i < kGroup; ++i) r.l += __expf(x[k][i] - base);
-    }
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) merge(r, shfl_xor(r, off));
-    if (lane == 0) warp_rec[warp] = r;
+// A CTA's records into one, in every lane of warp 0; `of_warps` has a place for each warp.
+template <int WARPS>
+__device__ __forceinline__ void merge_block(Record &r, Record *of_warps) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    merge_warp(r);
+    __syncthreads();   // (the records of the row before have been read)
+    if (lane == 0) of_warps[warp] = r;
     __syncthreads();
     if (warp != 0) return;
-    r = warp_rec[lane & (kLogitsThreads / 32 - 1)];
-    if (lane >= kLogitsThreads / 32) { r.m = -INFINITY; r.l = 0.f; r.token = -1; }
+    r = of_warps[lane & (WARPS - 1)];
+    if (lane >= WARPS) none_yet(r);
+    merge_warp(r);
+}
+
+// a group of elements, as they are and as floats
+template <typename T> struct Group;
+template <> struct Group<float> {
+    float4 a;
+    __device__ __forceinline__ void load(const float *p) { a = *reinterpret_cast<const float4 *>(p); }
+    __device__ __forceinline__ void unpack(float (&x)[kGroup]) const { x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; }
+};
+template <> struct Group<__nv_bfloat16> {
+    uint2 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = *reinterpret_cast<const uint2 *>(p); }
+    __device__ __forceinline__ void unpack(float (&x)[kGroup]) const {
+        x[0] = __uint_as_float(a.x << 16); x[1] = __uint_as_float(a.x & 0xffff0000u);
+        x[2] = __uint_as_float(a.y << 16); x[3] = __uint_as_float(a.y & 0xffff0000u);
+    }
+};
+
+// x / t, correctly rounded.  With r = 1 / t correctly rounded and q = x r within a unit in the last place of the quotient,
+// fma(fma(-q, t, x), r, q) is the correctly rounded quotient (Markstein, 1990), as long as nothing leaves the normal
+// numbers: otherwise the division itself.
+// (One element of N far from 1 sends them all the long way.)
+__device__ __noinline__ float divided_slowly(float x, float t) { return __fdiv_rn(x, t); }
+template <int N>
+__device__ __forceinline__ void divide(float (&x)[N][kGroup], float t, float r) {
+    bool plain = r != 0.f;
 #pragma unroll
-    for (int off = kLogitsThreads / 64; off >= 1; off >>= 1) merge(r, shfl_xor(r, off));
-    Record *slots = a.records + (size_t)row * a.slices;
-    if (a.slices > 1) {
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) plain = plain && fabsf(x[k][i]) < 1e25f && fabsf(x[k][i]) > 1e-25f;
+    if (plain) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) {
+                const float q = x[k][i] * r;
+                x[k][i] = fmaf(fmaf(-q, t, x[k][i]), r, q);
+            }
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) x[k][i] = divided_slowly(x[k][i], t);
+    }
+}
+
+// The best of a group's four (y = x + noise) where it beats what the thread has.
+__device__ __forceinline__ void best_of(Record &r, const float (&x)[kGroup], float y0, float y1, float y2, float y3, int t0) {
+    const float top = fmaxf(fmaxf(y0, y1), fmaxf(y2, y3));   // (passes NaN over)
+    if (top > r.best) {
+        const int i = y0 == top ? 0 : y1 == top ? 1 : y2 == top ? 2 : 3;
+        r.best = top;
+        r.best_x = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
+        r.token = t0 + i;
+    }
+}
+
+template <typename T, int PER>
+__global__ void __launch_bounds__(kLogitsThreads, kLogitsCtas)
+logits_kernel(const LogitsArgs a) {
+    constexpr int kPc = kPiece<PER>, kWarps = kLogitsThreads / 32;
+    static_assert(kPc <= 65536 && kPc % (4 * kLogitsThreads) == 0 && kPc / 32 <= kLogitsThreads, "16 bits a listed token; cleared by fours; a word a thread");
+    const arb_logits_params &p = a.p;
+    extern __shared__ __align__(16) int counts[];         // [kPc] counters, then the tokens' x; [kPc] listed tokens; a bit per token
+    uint16_t *list = reinterpret_cast<uint16_t *>(counts + kPc);
+    uint32_t *touched = reinterpret_cast<uint32_t *>(list + kPc);
+    float *xs = reinterpret_cast<float *>(counts);
+    __shared__ Record warp_rec[kWarps];
+    __shared__ int listed;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = p.vocab, row = blockIdx.y, runs = gridDim.x;
+    const bool special = p.history || p.bias_offsets, wanted = p.tokens || p.logprobs;
+    const T *x_in = static_cast<const T *>(p.logits) + row * (p.logits_stride ? p.logits_stride : (long long)V);
+    // groups start where the logits' own alignment has them; the dense fp32 arrays' groups agree or are taken one by one
+    const int skew = (int)((reinterpret_cast<uintptr_t>(x_in) / sizeof(T)) & (kGroup - 1));
+    const int piece_begin = (int)((long long)a.pieces * blockIdx.x / runs), piece_end = (int)((long long)a.pieces * (blockIdx.x + 1) / runs);
+    auto fetch = [&](int from, int to) {   // pieces into L2 (before the kernel ahead has ended, too: L2 holds what it then writes)
+        const long long first = max(from * kPc - skew, 0), tokens = min((long long)to * kPc - skew, (long long)V) - first;
+        prefetch_l2(x_in + first, tokens * (long long)sizeof(T));
+        if (p.noise) prefetch_l2(p.noise + (size_t)row * V + first, tokens * 4);
+    };
+    let_successor_start();
+    if (tid == 0) fetch(piece_begin, min(piece_begin + 2, piece_end));
+    if (special) {   // all zero at the start of a piece
+#pragma unroll
+        for (int i = 0; i < kPc / 4 / kLogitsThreads; ++i) reinterpret_cast<uint4 *>(counts)[i * kLogitsThreads + tid] = make_uint4(0, 0, 0, 0);
+        if (tid < kPc / 32) touched[tid] = 0;
+        if (tid == 0) listed = 0;
+        __syncthreads();
+    }
+    wait_for_predecessor();
+    const float temperature = p.temperature ? p.temperature[row] : 1.0f;
+    const bool scaled = p.temperature && temperature > 0.f;
+    const float per_temperature = temperature > 1e-6f && temperature < 1e6f ? __frcp_rn(temperature) : 0.f;
+    const float *noise = p.noise && temperature > 0.f ? p.noise + (size_t)row * V : nullptr;
+    float *out = p.out ? p.out + (size_t)row * V : nullptr;
+    const uint32_t *mask = p.mask ? p.mask + (size_t)row * p.mask_stride : nullptr;
+    const bool noise_alike = noise && (int)((reinterpret_cast<uintptr_t>(noise) / 4) & 3) == skew;
+    const bool out_alike = out && (int)((reinterpret_cast<uintptr_t>(out) / 4) & 3) == skew;
+    Record r;
+    none_yet(r);
+
+    int n_history = 0, b_begin = 0, b_end = 0;
+    float repetition = 1.f, presence = 0.f, frequency = 0.f;
+    if (p.history) {
+        if (p.repetition) repetition = p.repetition[row];
+        if (p.presence) presence = p.presence[row];
+        if (p.frequency) frequency = p.frequency[row];
+    }
+    if (p.history) n_history = p.history_lens ? max(0, min(p.history_lens[row], p.history_stride)) : p.history_stride;
+    if (p.bias_offsets) {
+        b_begin = max(0, min(p.bias_offsets[row], p.bias_total));
+        b_end = max(b_begin, min(p.bias_offsets[row + 1], p.bias_total));
+    }
+    const bool alike = (!noise || noise_alike) && (!out || out_alike);
+#pragma unroll 1
+    for (int piece = piece_begin; piece < piece_end; ++piece) {
+    const int lo = piece * kPc - skew;   // first token of the piece (below 0: the row starts inside a group)
+    if (tid == 0 && piece + 2 < piece_end) fetch(piece + 2, piece + 3);
+
+    // ---- which tokens of the piece are special
+    bool again = false;   // a token is listed twice among the biases
+    int n_listed = 0;
+    auto mine = [&](int t) { return (unsigned)(t - lo) < (unsigned)kPc && (unsigned)t < (unsigned)V; };
+    if (special) {
+        // Counts the tokens of a thread, kHeld of them, all atomics in flight together, and lists those not met before; a whole
+        // warp is here.
+        auto all_of = [&](const int32_t *tokens, int n, int one) {
+            for (int i0 = 0; i0 < n; i0 += kHeld * kLogitsThreads) {
+                int t[kHeld];
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k) {
+                    const int i = i0 + k * kLogitsThreads + tid;
+                    t[k] = i < n ? __ldg(tokens + i) : -1;
+                }
+                uint32_t begun = 0;
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k) {
+                    if (mine(t[k])) {
+                        const int old = atomicAdd(&counts[t[k] - lo], one);
+                        if (old == 0) begun |= 1u << k;
+                        again = again || old >= kBiasOne;
+                    }
+                }
+                if (!__any_sync(0xffffffffu, begun != 0)) continue;
+                int before = __popc(begun);
+                const int own = before;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const int other = __shfl_up_sync(0xffffffffu, before, off);
+                    if (lane >= off) before += other;
+                }
+                int at = 0;
+                if (lane == 31) at = atomicAdd(&listed, before);
+                at = __shfl_sync(0xffffffffu, at, 31) + before - own;
+#pragma unroll
+                for (int k = 0; k < kHeld; ++k) {
+                    if (begun >> k & 1u) {
+                        list[at++] = (uint16_t)(t[k] - lo);
+                        atomicOr(&touched[(t[k] - lo) >> 5], 1u << ((t[k] - lo) & 31));
+                    }
+                }
+            }
+        };
+        all_of(p.history + (size_t)row * p.history_stride, n_history, 1);
+        all_of(p.bias_tokens + b_begin, b_end - b_begin, kBiasOne);
+        again = __syncthreads_or(again);
+        n_listed = listed;
+        for (int i = tid; i < n_listed; i += kLogitsThreads) {
+            const int at = list[i], c = counts[at] & (kBiasOne - 1);
+            float v = Elt<T>::to_float(x_in[lo + at]);
+            if (c > 0) {
+                v = v > 0.f ? __fdiv_rn(v, repetition) : __fmul_rn(v, repetition);
+                v = __fsub_rn(v, presence);
+                v = __fsub_rn(v, __fmul_rn(frequency, (float)c));
+            }
+            xs[at] = v;
+        }
+        __syncthreads();
+        for (int i = b_begin + tid; i < b_end; i += kLogitsThreads) {
+            const int t = __ldg(p.bias_tokens + i);
+            if (!mine(t)) continue;
+            float sum = __ldg(p.bias_values + i);
+            if (again) {
+                bool first = true;
+                for (int j = b_begin; j < i && first; ++j) first = __ldg(p.bias_tokens + j) != t;
+                if (!first) continue;
+                for (int j = i + 1; j < b_end; ++j)
+                    if (__ldg(p.bias_tokens + j) == t) sum = __fadd_rn(sum, __ldg(p.bias_values + j));
+            }
+            xs[t - lo] = __fadd_rn(xs[t - lo], sum);
+        }
+        if (p.bias_offsets) __syncthreads();
+    }
+
+    // ---- the stream, compiled twice: every group of the piece whole and alike in all arrays, or with a look at each.  What a row
+    //      does not use costs a branch per piece, not an instruction per token.
+    auto stream = [&](auto inner_c) {
+        constexpr bool kInner = decltype(inner_c)::value;
+        constexpr int kStep = kLogitsThreads * kGroup;
+        auto whole = [&](int t0) { return kInner || (t0 >= 0 && t0 + kGroup <= V); };
+        const int t_first = lo + tid * kGroup, w_last = (V - 1) >> 5;   // group k: kStep tokens on
+        Group<T> raw[PER];
+        Group<float> nz[PER];
+        float x[PER][kGroup];
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (whole(t_first + k * kStep)) raw[k].load(x_in + t_first + k * kStep);
+        if (noise) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (kInner || (noise_alike && whole(t_first + k * kStep))) nz[k].load(noise + t_first + k * kStep);
+        }
+        uint32_t hide[PER];   // of a group: tokens that are not allowed, or not there
+#pragma unroll
+        for (int k = 0; k < PER; ++k) hide[k] = 0;
+        if (mask) {   // t0 may lie below 0 and the bits in two words
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int t0 = t_first + k * kStep, w = kInner ? t0 >> 5 : max(t0, 0) >> 5;
+                const uint32_t w0 = __ldg(mask + (kInner ? w : min(w, w_last))), w1 = __ldg(mask + min(w + 1, w_last));
+                hide[k] = ~(kInner || t0 >= 0 ? __funnelshift_r(w0, w1, t0 & 31) : w0 << -t0);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) raw[k].unpack(x[k]);
+        if (!kInner) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int t0 = t_first + k * kStep;
+                if (whole(t0)) continue;
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) {
+                    const bool real = (unsigned)(t0 + i) < (unsigned)V;
+                    x[k][i] = real ? Elt<T>::to_float(x_in[t0 + i]) : 0.f;
+                    if (!real) hide[k] |= 1u << i;
+                }
+            }
+        }
+        if (special) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int at = t_first + k * kStep - lo;
+                const uint32_t those = touched[at >> 5] >> (at & 31);
+                if (those & ((1u << kGroup) - 1u)) {
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i)
+                        if (those & (1u << i)) x[k][i] = xs[at + i];
+                }
+            }
+        }
+        if (scaled) divide(x, temperature, per_temperature);
+        if (!kInner || mask) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i)
+                    if (hide[k] & (1u << i)) x[k][i] = -INFINITY;
+        }
+        if (out) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int t0 = t_first + k * kStep;
+                if (kInner || (out_alike && whole(t0))) {
+                    *reinterpret_cast<float4 *>(out + t0) = make_float4(x[k][0], x[k][1], x[k][2], x[k][3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i)
+                        if ((unsigned)(t0 + i) < (unsigned)V) out[t0 + i] = x[k][i];
+                }
+            }
+        }
+        if (!wanted) return;
+        float m = r.m;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) m = fmaxf(fmaxf(fmaxf(m, x[k][0]), fmaxf(x[k][1], x[k][2])), x[k][3]);   // (passes NaN over)
+        const float base = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) l += __expf(x[k][i] - base);   // (scaled before the difference, the type's lowest value would overflow)
+        r.l = r.l * __expf(r.m - base) + l;
+        r.m = m;
+        if (noise) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int t0 = t_first + k * kStep;
+                float n[kGroup];
+                nz[k].unpack(n);
+                if (!kInner && !(noise_alike && whole(t0))) {
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i) n[i] = (unsigned)(t0 + i) < (unsigned)V ? noise[t0 + i] : 0.f;
+                }
+                best_of(r, x[k], __fadd_rn(x[k][0], n[0]), __fadd_rn(x[k][1], n[1]), __fadd_rn(x[k][2], n[2]), __fadd_rn(x[k][3], n[3]), t0);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) best_of(r, x[k], x[k][0], x[k][1], x[k][2], x[k][3], t_first + k * kStep);
+        }
+    };
+    if (alike && lo >= 0 && lo + kPc <= V) stream(std::true_type());
+    else stream(std::false_type());
+
+    if (special && piece + 1 < piece_end) {
+        __syncthreads();   // (everyone has read what it needs of the piece)
+        for (int i = tid; i < n_listed; i += kLogitsThreads) counts[list[i]] = 0;
+        if (tid < kPc / 32) touched[tid] = 0;
+        if (tid == 0) listed = 0;
+        __syncthreads();
+    }
+    }
+    if (!wanted) return;
+    merge_block<kWarps>(r, warp_rec);
+    if (warp != 0) return;
+    if (runs > 1) {
+        Record *records = a.records + (size_t)row * runs;
+        bool last = false;
         if (lane == 0) {
-            slots[blockIdx.x] = r;
+            records[blockIdx.x] = r;
             __threadfence();
-            last = atomicAdd(&a.counters[row], 1) == a.slices - 1;
-            if (last) a.counters[row] = 0;   // every slice has arrived: ready for the next call
+            last = atomicAdd(&a.counters[row], 1) == runs - 1;
+            if (last) a.counters[row] = 0;   // every run has arrived: ready for the next call
             __threadfence();
         }
-        __syncwarp();
-        if (!last) return;
-        r.m = -INFINITY; r.l = 0.f; r.best = -INFINITY; r.best_x = -INFINITY; r.token = -1;
-        for (int i = lane; i < a.slices; i += 32) {
-            const float4 f = __ldcg(reinterpret_cast<const float4 *>(slots + i));
+        if (!__shfl_sync(0xffffffffu, (int)last, 0)) return;
+        none_yet(r);
+        for (int i = lane; i < runs; i += 32) {
+            const float4 f = __ldcg(reinterpret_cast<const float4 *>(records + i));
             Record o;
             o.m = f.x; o.l = f.y; o.best = f.z; o.best_x = f.w;
-            o.token = __ldcg(&slots[i].token);
+            o.token = __ldcg(&records[i].token);
             merge(r, o);
         }
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) merge(r, shfl_xor(r, off));
+        merge_warp(r);
     }
     if (lane == 0) {
         if (p.tokens) p.tokens[row] = r.token;
@@ -246,22 +449,35 @@ logits_kernel(const LogitsArgs a) {
     }
 }
 
+// (a row may start up to three elements into a group)
+inline int pieces_of(int vocab, int piece) { return (int)(((long long)vocab + kGroup - 1 + piece - 1) / piece); }
+
+template <typename T, int PER>
+arb_status launch_typed(Ctx *ctx, LogitsArgs a, cudaStream_t stream) {
+    constexpr int kPc = kPiece<PER>;
+    constexpr int kSmem = kPc * (int)(sizeof(int) + sizeof(uint16_t)) + kPc / 8;   // of a call with history or biases
+    static_assert(kSmem <= 48 * 1024, "no opt-in needed");
+    a.pieces = pieces_of(a.p.vocab, kPc);
+    const long long share = (long long)ctx->num_sms * kLogitsCtas / a.p.rows;
+    const int runs = (int)(share < 1 ? 1 : share < a.pieces ? share : a.pieces);   // of a row
+    if ((size_t)a.p.rows * runs * sizeof(Record) > ctx->chunk_ws_bytes) return ARB_ERR_WORKSPACE;
+    const cudaError_t err = launch_pdl(logits_kernel<T, PER>, dim3(runs, a.p.rows), dim3(kLogitsThreads),
+                                       a.p.history || a.p.bias_offsets ? kSmem : 0, stream, a);
+    ctx->launches++;
+    return err == cudaSuccess ? ARB_OK : ARB_ERR_CUDA;
+}
+
 }  // namespace
 
 arb_status launch_logits(Ctx *ctx, const arb_logits_params &p, cudaStream_t stream) {
     LogitsArgs a;
     a.p = p;
-    a.slices = (p.vocab + kGroup - 1 + kSlice - 1) / kSlice;   // a row may start up to seven elements into a group
     a.records = reinterpret_cast<Record *>(ctx->chunk_ws);
     a.counters = ctx->counters;
-    if ((p.tokens || p.logprobs) && (size_t)p.rows * a.slices * sizeof(Record) > ctx->chunk_ws_bytes) return ARB_ERR_WORKSPACE;
-    const size_t smem = sizeof(int) * kSlice * ((p.history ? 1 : 0) + (p.bias_offsets ? 1 : 0));
-    const dim3 grid(a.slices, p.rows);
-    const cudaError_t err = p.dtype == ARB_BF16
-                                ? launch_pdl(logits_kernel<__nv_bfloat16>, grid, dim3(kLogitsThreads), smem, stream, a)
-                                : launch_pdl(logits_kernel<float>, grid, dim3(kLogitsThreads), smem, stream, a);
-    ctx->launches++;
-    return err == cudaSuccess ? ARB_OK : ARB_ERR_CUDA;
+    // smaller pieces where they still find a CTA each
+    const bool few = (long long)p.rows * pieces_of(p.vocab, kPiece<2>) <= (long long)ctx->num_sms * kLogitsCtas;
+    if (p.dtype == ARB_BF16) return few ? launch_typed<__nv_bfloat16, 2>(ctx, a, stream) : launch_typed<__nv_bfloat16, 4>(ctx, a, stream);
+    return few ? launch_typed<float, 2>(ctx, a, stream) : launch_typed<float, 4>(ctx, a, stream);
 }
 
 }  // namespace arb

@@ -4,10 +4,12 @@
 // Plain memory movement with some arithmetic on the way: every row is read once and written once, (Hq + 2 Hkv) D elements a
 // token each way.  A row of D values is held by D / 8 neighbouring lanes, eight values each, as two vectors of four that hold
 // both members of four rotation pairs: (p .. p + 3, p + rot / 2 ..) or eight neighbours, so that no lane needs another's
-// values to rotate.  The rows of one token share their four angles per lane: a lane group takes several heads of a token in
-// turn and works out sines and cosines once (position times frequency in 64 bits, reduced to a turn, then sincospif: the
-// error of an angle does not grow with the position), four rows in flight.
+// values to rotate.  The rows of one token share their four angles per lane: a warp takes neighbouring heads of a token, works
+// out sines and cosines once (position times frequency in 64 bits, reduced to a part of a turn: the error of an angle does not
+// grow with the position) and goes through its rows kind by kind, so that the lane groups of a warp never part ways.
 #include "arb_append.cuh"
+
+#include <type_traits>
 
 namespace arb {
 
@@ -30,6 +32,7 @@ struct RopeArgs {
 };
 
 constexpr int kRopeRows = 4;   // rows of a lane group in flight
+constexpr int kRopeCtas = 3;   // resident CTAs of an SM
 
 template <typename T> struct Four;
 template <> struct Four<float> { using V = uint4; };
@@ -72,11 +75,12 @@ __device__ __forceinline__ void store_i4_halves(char *row, const float (&x)[8], 
 }
 
 template <typename T, int D, Kv KV, bool INTER>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, kRopeCtas)
 rope_append_kernel(const RopeArgs r) {
     using V = typename Four<T>::V;
     constexpr int kLanes = D / 8;                       // lanes of a row
-    constexpr int kGroups = kAppendThreads / kLanes;    // lane groups of a CTA
+    constexpr int kGroups = 32 / kLanes;                // lane groups of a warp: neighbouring heads of a token
+    constexpr int kRowBytes = D * (int)sizeof(T);
     extern __shared__ int asm_[];
     const AppendArgs &a = r.a;
     pdl_enter();
@@ -89,11 +93,36 @@ rope_append_kernel(const RopeArgs r) {
         off0 = turns ? p0 : r.rot + (p0 - r.rot / 2);
         off1 = off0 + (turns ? r.rot / 2 : (D - r.rot) / 2);
     }
-    const int heads = r.Hq + 2 * a.Hkv;
-    const long long units = (long long)min(pl.pref[a.batch], a.total_new) * r.units_per_token;
-    for (long long u = (long long)blockIdx.x * kGroups + threadIdx.x / kLanes; u < units; u += (long long)gridDim.x * kGroups) {
-        const int tok = (int)(u / r.units_per_token), h_begin = (int)(u - (long long)tok * r.units_per_token) * r.heads_per_unit;
+    const int heads = r.Hq + 2 * a.Hkv, mine = (threadIdx.x & 31) / kLanes;   // this lane's group of the warp
+    const unsigned units = (unsigned)min(pl.pref[a.batch], a.total_new) * (unsigned)r.units_per_token;
+    const unsigned warps = gridDim.x * (kAppendThreads / 32);
+    for (unsigned u = blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32; u < units; u += warps) {
+        const int tok = (int)(u / (unsigned)r.units_per_token), h_begin = ((int)u - tok * r.units_per_token) * r.heads_per_unit;
         const int h_end = min(h_begin + r.heads_per_unit, heads);
+        // Rows h .. seg_end - 1 of the unit (the same for the whole warp) are of one kind (0: queries, 1: keys, 2: values) and lie D elements apart.  The first
+        // rows are asked for before anything else is looked up.
+        int h = h_begin, kind, seg_end;
+        const char *src;
+        auto aim = [&]() {
+            const int k_begin = r.Hq, v_begin = r.Hq + a.Hkv;
+            kind = (h >= k_begin) + (h >= v_begin);
+            seg_end = min(h_end, kind == 0 ? k_begin : kind == 1 ? v_begin : heads);
+            src = kind == 0 ? r.q + tok * r.q_stride : kind == 1 ? a.k_new + tok * r.k_stride : a.v_new + tok * r.v_stride;
+            src += (h - (kind == 0 ? 0 : kind == 1 ? k_begin : v_begin) + mine) * kRowBytes;
+        };
+        V raw[kRopeRows][2];
+        auto load = [&]() {
+            const char *at0 = src + off0 * (int)sizeof(T), *at1 = src + off1 * (int)sizeof(T);
+#pragma unroll
+            for (int k = 0; k < kRopeRows; ++k) {
+                if (h + k * kGroups + mine < seg_end) {
+                    raw[k][0] = *reinterpret_cast<const V *>(at0 + k * kGroups * kRowBytes);
+                    raw[k][1] = *reinterpret_cast<const V *>(at1 + k * kGroups * kRowBytes);
+                }
+            }
+        };
+        aim();
+        load();
         int b = 0, hi = a.batch;
         while (hi - b > 1) {
             const int mid = (b + hi) >> 1;
@@ -101,101 +130,101 @@ rope_append_kernel(const RopeArgs r) {
         }
         const bool okay = pl.okay[b];
         const int place = okay ? pl.start[b] + (tok - pl.pref[b]) : 0;
-        const long long slot = okay ? (long long)a.block_table[(size_t)b * a.max_pages + place / kPage] * a.Hkv * kPage + place % kPage : 0;
+        long long slot = okay ? (long long)a.block_table[(size_t)b * a.max_pages + place / kPage] * a.Hkv * kPage + place % kPage : 0;
+        if (!ARB_IN_RANGE(a.status, slot, (long long)a.num_pages * a.Hkv * kPage - (a.Hkv - 1) * kPage)) slot = 0;
         float c[4], s[4];
-        if (turns && h_begin < r.Hq + a.Hkv) {
+        if (turns && kind < 2) {
             const double pos = (double)(r.positions ? r.positions[tok] : place) * 0.15915494309189533577;   // 1 / (2 pi): in turns
             const float4 f = __ldg(reinterpret_cast<const float4 *>(r.inv_freq + p0));
             const float ff[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const double t = pos * (double)ff[i];
-                sincospif(2.0f * (float)(t - rint(t)), &s[i], &c[i]);
+                const float part = (float)(t - rint(t));   // -0.5 .. 0.5 of a turn
+                if constexpr (sizeof(T) == 4) {
+                    sincospif(2.0f * part, &s[i], &c[i]);
+                } else {   // 2^-20 absolute, where the rows are known to 2^-9
+                    __sincosf(6.2831853071795865f * part, &s[i], &c[i]);
+                }
             }
         }
-        for (int h0 = h_begin; h0 < h_end; h0 += kRopeRows) {
-            V raw[kRopeRows][2];
-#pragma unroll
-            for (int k = 0; k < kRopeRows; ++k) {
-                const int h = min(h0 + k, h_end - 1);
-                const char *src = h < r.Hq ? r.q + tok * r.q_stride + (size_t)h * D * sizeof(T)
-                                : h < r.Hq + a.Hkv ? a.k_new + tok * r.k_stride + (size_t)(h - r.Hq) * D * sizeof(T)
-                                                   : a.v_new + tok * r.v_stride + (size_t)(h - r.Hq - a.Hkv) * D * sizeof(T);
-                raw[k][0] = *reinterpret_cast<const V *>(src + off0 * sizeof(T));
-                raw[k][1] = *reinterpret_cast<const V *>(src + off1 * sizeof(T));
+        // kRopeRows rows of one kind, which is a constant of each instance
+        auto rows = [&](auto kind_c) {
+            constexpr int K = decltype(kind_c)::value;
+            float w[8];
+            const float *weight = K == 0 ? r.q_weight : r.k_weight;
+            const bool norm = K < 2 && weight != nullptr;
+            if (norm) {
+                const float4 w0 = __ldg(reinterpret_cast<const float4 *>(weight + off0)), w1 = __ldg(reinterpret_cast<const float4 *>(weight + off1));
+                w[0] = w0.x; w[1] = w0.y; w[2] = w0.z; w[3] = w0.w; w[4] = w1.x; w[5] = w1.y; w[6] = w1.z; w[7] = w1.w;
             }
+            const int head = (K == 0 ? h : K == 1 ? h - r.Hq : h - r.Hq - a.Hkv) + mine;   // of its kind
+            constexpr int kOutRow = K == 0 || KV == Kv::kSame ? kRowBytes : KV == Kv::kE4m3 ? D : D / 2;   // bytes
+            constexpr int kOutStep = kGroups * (K == 0 ? kOutRow : kPage * kOutRow);                        // from row to row of the lane
+            const long long row0 = K == 0 ? (long long)tok * r.Hq + head : slot + (long long)head * kPage;
+            char *dst = (K == 0 ? r.q_out : K == 1 ? a.k_pages : a.v_pages) + row0 * kOutRow;
 #pragma unroll
             for (int k = 0; k < kRopeRows; ++k) {
-                const int h = h0 + k;   // (everything up to the stores is the same for the lanes of a group)
-                if (h >= h_end) break;
-                const bool is_q = h < r.Hq, is_v = h >= r.Hq + a.Hkv;
-                if (!okay && !is_q) continue;
+                if (h + k * kGroups + mine >= seg_end) continue;   // (the same for the lanes of a group)
                 float x[8];
                 unpack4(raw[k][0], x);
                 unpack4(raw[k][1], x + 4);
-                if (!is_v) {
-                    const float *w = is_q ? r.q_weight : r.k_weight;
-                    if (w != nullptr) {
-                        float ss = 0.f;
+                if (norm) {
+                    float ss = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+                    for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
-                        for (int off = kLanes / 2; off >= 1; off >>= 1) ss += __shfl_xor_sync(group_mask, ss, off);
-                        const float inv = rsqrtf(ss * (1.0f / D) + r.eps);
-                        const float4 w0 = __ldg(reinterpret_cast<const float4 *>(w + off0));
-                        const float4 w1 = __ldg(reinterpret_cast<const float4 *>(w + off1));
-                        x[0] *= inv * w0.x; x[1] *= inv * w0.y; x[2] *= inv * w0.z; x[3] *= inv * w0.w;
-                        x[4] *= inv * w1.x; x[5] *= inv * w1.y; x[6] *= inv * w1.z; x[7] *= inv * w1.w;
-                    }
-                    if (turns) {
+                    for (int off = kLanes / 2; off >= 1; off >>= 1) ss += __shfl_xor_sync(group_mask, ss, off);
+                    const float inv = rsqrtf(ss * (1.0f / D) + r.eps);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float &e = INTER ? x[2 * i] : x[i], &o = INTER ? x[2 * i + 1] : x[4 + i];
-                            const float y = e * c[i] - o * s[i];
-                            o = e * s[i] + o * c[i];
-                            e = y;
-                        }
+                    for (int i = 0; i < 8; ++i) x[i] *= inv * w[i];
+                }
+                if (K < 2 && turns) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float &e = INTER ? x[2 * i] : x[i], &o = INTER ? x[2 * i + 1] : x[4 + i];
+                        const float y = e * c[i] - o * s[i];
+                        o = e * s[i] + o * c[i];
+                        e = y;
                     }
                 }
-                if (is_q) {
-                    char *dst = r.q_out + ((size_t)tok * r.Hq + h) * D * sizeof(T);
-                    V y0 = {}, y1 = {};
-                    if (okay) { pack4(x, y0); pack4(x + 4, y1); }   // (a refused sequence: rows of zeros)
-                    *reinterpret_cast<V *>(dst + off0 * sizeof(T)) = y0;
-                    *reinterpret_cast<V *>(dst + off1 * sizeof(T)) = y1;
-                    continue;
-                }
-                const int kvh = is_v ? h - r.Hq - a.Hkv : h - r.Hq;
-                const long long row = slot + (long long)kvh * kPage;
-                if (!ARB_IN_RANGE(a.status, row, (long long)a.num_pages * a.Hkv * kPage)) continue;
-                char *pool = is_v ? a.v_pages : a.k_pages;
-                if constexpr (KV == Kv::kSame) {
-                    char *dst = pool + (size_t)row * D * sizeof(T);
+                char *at = dst + k * kOutStep;
+                if constexpr (K == 0 || KV == Kv::kSame) {
                     V y0 = raw[k][0], y1 = raw[k][1];   // values bit for bit
-                    if (!is_v) { pack4(x, y0); pack4(x + 4, y1); }
-                    *reinterpret_cast<V *>(dst + off0 * sizeof(T)) = y0;
-                    *reinterpret_cast<V *>(dst + off1 * sizeof(T)) = y1;
+                    if (K < 2) { pack4(x, y0); pack4(x + 4, y1); }
+                    if (K == 0 && !okay) y0 = y1 = V{};   // (a refused sequence: rows of zeros)
+                    *reinterpret_cast<V *>(at + off0 * (int)sizeof(T)) = y0;
+                    *reinterpret_cast<V *>(at + off1 * (int)sizeof(T)) = y1;
                 } else if constexpr (KV == Kv::kE4m3) {
-                    const float scale = is_v ? r.v_inv_scale : r.k_inv_scale;
-                    char *dst = pool + (size_t)row * D;
-                    *reinterpret_cast<uint32_t *>(dst + off0) = e4m3x4(x, scale);
-                    *reinterpret_cast<uint32_t *>(dst + off1) = e4m3x4(x + 4, scale);
+                    const float scale = K == 1 ? r.k_inv_scale : r.v_inv_scale;
+                    *reinterpret_cast<uint32_t *>(at + off0) = e4m3x4(x, scale);
+                    *reinterpret_cast<uint32_t *>(at + off1) = e4m3x4(x + 4, scale);
                 } else {
                     float m = 0.f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
 #pragma unroll
                     for (int off = kLanes / 2; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(group_mask, m, off));
-                    char *dst = pool + (size_t)row * (D / 2);
                     float scale;
                     if constexpr (INTER) {
-                        *reinterpret_cast<uint32_t *>(dst + l * 4) = i4_word(x, m, scale);
+                        *reinterpret_cast<uint32_t *>(at + l * 4) = i4_word(x, m, scale);
                     } else {
                         scale = m > 0.f ? __fdiv_rn(m, 7.f) : 0.f;
-                        store_i4_halves(dst, x, m > 0.f ? __fdiv_rn(7.f, m) : 0.f, off0, off1, group_mask);
+                        store_i4_halves(at, x, m > 0.f ? __fdiv_rn(7.f, m) : 0.f, off0, off1, group_mask);
                     }
-                    if (l == 0) (is_v ? r.v_scales : r.k_scales)[row] = scale;
+                    if (l == 0) (K == 1 ? r.k_scales : r.v_scales)[row0 + (long long)k * kGroups * kPage] = scale;
                 }
+            }
+        };
+        while (h < h_end) {
+            if (kind == 0) rows(std::integral_constant<int, 0>());
+            else if (okay && kind == 1) rows(std::integral_constant<int, 1>());
+            else if (okay) rows(std::integral_constant<int, 2>());
+            h = min(h + kRopeRows * kGroups, seg_end);
+            src += kRopeRows * kGroups * kRowBytes;
+            if (h < h_end) {
+                if (h == seg_end) aim();
+                load();
             }
         }
     }
@@ -264,12 +293,16 @@ arb_status launch_rope_append(Ctx *ctx, const arb_attn_params &p, const arb_rope
     r.eps = rope.eps;
     r.Hq = p.num_q_heads;
     r.rot = rope.rot_dim;
-    // A lane group takes as many rows of a token as leave every resident group a share (a row each in small calls).
-    const int heads = p.num_q_heads + 2 * p.num_kv_heads, groups = kAppendThreads / (D / 8);
-    const long long resident = (long long)ctx->num_sms * 4 * groups, rows = (long long)total_new * heads;
-    r.heads_per_unit = (int)(rows <= resident ? 1 : rows / resident < heads ? (rows + resident - 1) / resident : heads);
+    // A warp takes a row per lane group in a small call, and in a large one so many heads of a token that eight shares remain
+    // for every resident warp: fewer and larger ones leave warps idle at the end, smaller ones work the angles out more often.
+    const int heads = p.num_q_heads + 2 * p.num_kv_heads, groups = 256 / D;
+    const long long resident = (long long)ctx->num_sms * kRopeCtas * (kAppendThreads / 32), rows = (long long)total_new * heads;
+    const int batch = kRopeRows * groups;
+    const long long share = (rows / (8 * resident) + batch) / batch * batch;
+    r.heads_per_unit = (int)(rows <= resident * groups ? groups : share < heads ? share : heads);
     r.units_per_token = (heads + r.heads_per_unit - 1) / r.heads_per_unit;
-    const long long want = ((long long)total_new * r.units_per_token + groups - 1) / groups, cap = (long long)ctx->num_sms * 4;
+    const long long want = ((long long)total_new * r.units_per_token * 32 + kAppendThreads - 1) / kAppendThreads,
+                    cap = (long long)ctx->num_sms * kRopeCtas;
     const int grid = (int)(want < 1 ? 1 : want > cap ? cap : want);
     const bool inter = rope.interleaved != 0;
     switch (cache) {

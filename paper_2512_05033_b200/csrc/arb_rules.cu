@@ -11,7 +11,10 @@ arb_status launch_attn_rules(Ctx *ctx, const arb_attn_params &p, const arb_score
                      rules.prefix_lens, rules.first_keys};
     // the host knows only the total and the maximum of q_lens
     if (p.max_q_len == 1 || p.total_q > p.max_q_len) {
-        const arb_status st = launch_decode_rules(ctx, p, r, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
+        // the single launch plans from lengths alone; documents' first keys and fp32 take the other kernel
+        const arb_status st = decode_step_supported(p) && !r.first_keys
+                                  ? launch_step_rules(ctx, p, r, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream)
+                                  : launch_decode_rules(ctx, p, r, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
         if (st != ARB_OK) return st;
     }
     if (p.max_q_len < 2) return ARB_OK;

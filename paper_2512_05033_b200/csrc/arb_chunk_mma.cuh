@@ -106,12 +106,13 @@ __host__ __device__ constexpr size_t slot_floats(int head_dim) { return (size_t)
 // unit take half the tensor time, so the second term is hidden under the exponentials, and the weights keep what the
 // CUDA-core kernel that served these chunks before kept (fp32, far below the rounding of the output).  Measured: the
 // step-scoring batch with 64-dimension heads 14.1 ms -> 0.42 ms, a batch of 16 short steps over 1k-8k keys 1.33 ms -> 0.09 ms.
-template <int HD>
+// RULED: P is one bf16 term at either head dimension (prompts of documents, 32 / 8 heads of 64: 409 -> 278 us).
+template <int HD, bool RULED = false>
 struct Shape {
     static constexpr int kHalves = HD / 64;                       // 128-byte-swizzled 64-dimension pieces of a row
     static constexpr int kTileBytes = kHalves * kHalfBytes;       // [128 x HD] bf16
     static constexpr int kStages = HD == 64 ? 4 : 2;
-    static constexpr bool kSplitP = HD == 64;
+    static constexpr bool kSplitP = HD == 64 && !RULED;
     static constexpr uint32_t kPCols = kSplitP ? kBN : kBN / 2;   // two keys per column, hi then lo
     static constexpr uint32_t kOCol = kPCol + 2 * kPCols;
     static constexpr size_t kSlotFloats = slot_floats(HD);
@@ -141,7 +142,10 @@ struct MmaArgs {
 
 struct RuledArgs : MmaArgs {
     Rules rules;
+    float2 cap_fit[4];   // coefficients of the cap's polynomial in the square of the raw product, in both halves (see capped2)
+    int cap_plain;       // they are ordinary numbers
 };
+enum { kNoRules = 0, kRules = 1, kRulesBias = 2 };   // what a kernel is compiled for: ranges and cap; and slopes
 template <bool RULED>
 using ArgsOf = std::conditional_t<RULED, RuledArgs, MmaArgs>;
 
@@ -586,13 +590,34 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 
 // A row's 128 raw products of the keys key0 .. key0 + 127 become scores in log2 units.
 //
-// The cap.  While every product of the warp's rows lies within the cap (|s| <= cap, the common case: a cap is there for
-// outliers), x = s / cap stays within 1 and cap tanh(x) is s + s x^2 P(x^2): nine operations a score on the FMA pipe, two
-// scores an instruction, beside the exponential's one on the special-function unit (a tanh out of exponential and
-// reciprocal would make three there, and that unit is what a softmax group waits for already).  P is a least-maximum fit of
-// (tanh(x) / x - 1) / x^2 on [0, 1], relative error 7e-7: 5e-5 in the exponent at a cap of 50, a hundredth of the weights'
-// rounding to bf16.  Beyond the cap the exact form, tanh_any.
+// The cap.  While every product of the warp's rows lies within kCapPoly of the cap (the common case: a cap is there for
+// outliers), x = s / cap stays within it and cap tanh(x) is s + s x^2 P(x^2): operations of the FMA pipe, two scores an
+// instruction, beside the exponential's one on the special-function unit (a tanh out of exponential and reciprocal would make
+// three there, and that unit is what a softmax group waits for already).  P is a least-maximum fit of (tanh(x) / x - 1) / x^2 on
+// [0, 0.8], relative error 1.2e-6: 6e-5 in the exponent at a cap of 50, a fiftieth of the weights' rounding to bf16.
+// Beyond that the exact form, tanh_any.  A tile that all rows of the warp see whole, without a bias, takes the cap on the way to
+// the weights (see `weights`): tanh is monotonic, so the maximum is taken of the raw products.  The others, which have hidden
+// keys or a bias to take in between, get it here.  Step-scoring batch (32 steps, 28 / 4 heads, cap 30): polynomial of degree 5 in a
+// pass of its own 560 us, taken on the way to the weights with the scale folded in 480, with 208 registers a softmax thread
+// (see setmaxnreg below; 168 spill) 462; without a cap 323, arb_attn's kernel 285.  The FMA pipe's 7 operations for two scores and the
+// exponentials share the time; written in strict alternation they took as long.
 // The bias.  -slope |pos - j|; keys of a tile that lies at or before the row's own key are at distance pos - key0 - k.
+constexpr float kCapPoly = 0.8f;
+__device__ __forceinline__ uint64_t both(float x) { return pack_f32x2(x, x); }
+// Raw products r of two keys, |scale r| <= kCapPoly cap -> cap tanh(scale r / cap) log2 e plus add2: s + s x^2 P(x^2) with the powers of
+// scale / cap folded into the coefficients, s = scale log2 e r.  Seven operations for two keys.
+__device__ __forceinline__ uint64_t capped2(const RuledArgs &a, uint64_t r, uint64_t scale2, uint64_t add2) {
+    auto c = [&](int i) { return pack_f32x2(a.cap_fit[i].x, a.cap_fit[i].y); };
+    const uint64_t w = mul_f32x2(r, r);
+    uint64_t p = fma_f32x2(c(3), w, c(2));
+    p = fma_f32x2(p, w, c(1));
+    p = fma_f32x2(p, w, c(0));
+    return fma_f32x2(mul_f32x2(r, w), p, fma_f32x2(r, scale2, add2));
+}
+
+__device__ __forceinline__ uint64_t capped2(const MmaArgs &, uint64_t, uint64_t, uint64_t) { return 0; }   // (never called)
+
+template <bool BIAS>
 __device__ __forceinline__ void apply_rules(const RuledArgs &a, uint32_t (&v)[kBN], float slope_log2, int pos, int key0) {
     const bool capped = a.rules.to_cap > 0.f;
     if (capped) {
@@ -604,46 +629,51 @@ __device__ __forceinline__ void apply_rules(const RuledArgs &a, uint32_t (&v)[kB
                 mx4[u] = max3(mx4[u], fabsf(__uint_as_float(v[k + 2 * u])), fabsf(__uint_as_float(v[k + 2 * u + 1])));
         }
         const float big = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.rules.to_cap;
-        if (__any_sync(0xffffffffu, big > 1.0f)) {
+        if (!a.cap_plain || __any_sync(0xffffffffu, big > kCapPoly)) {
 #pragma unroll
             for (int k = 0; k < kBN; ++k) v[k] = __float_as_uint(a.rules.cap_log2 * tanh_any(__uint_as_float(v[k]) * a.rules.to_cap));
         } else {
-            constexpr float kFit[5] = {-0.3333027958869934f, 0.1328849047422409f, -0.05176828056573868f, 0.016906404867768288f,
-                                       -0.0031265760771930218f};
-            const uint64_t tc = pack_f32x2(a.rules.to_cap, a.rules.to_cap), cl = pack_f32x2(a.rules.cap_log2, a.rules.cap_log2);
+            const uint64_t scale2 = both(a.scale_log2);
 #pragma unroll
             for (int k = 0; k < kBN; k += 2) {
-                const uint64_t x = mul_f32x2(pack_f32x2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), tc);
-                const uint64_t u = mul_f32x2(x, x), s = mul_f32x2(x, cl);
-                uint64_t p = fma_f32x2(pack_f32x2(kFit[4], kFit[4]), u, pack_f32x2(kFit[3], kFit[3]));
-#pragma unroll
-                for (int i = 2; i >= 0; --i) p = fma_f32x2(p, u, pack_f32x2(kFit[i], kFit[i]));
                 float lo, hi;
-                unpack_f32x2(fma_f32x2(mul_f32x2(s, u), p, s), lo, hi);
+                unpack_f32x2(capped2(a, pack_f32x2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale2, 0ull), lo, hi);
                 v[k] = __float_as_uint(lo);
                 v[k + 1] = __float_as_uint(hi);
             }
         }
     }
-    if (a.rules.slopes) {
+    if (BIAS && a.rules.slopes) {
         const float sc = capped ? 1.0f : a.scale_log2;
         if (__any_sync(0xffffffffu, key0 + kBN - 1 > pos)) {
 #pragma unroll
             for (int k = 0; k < kBN; ++k)
                 v[k] = __float_as_uint(fmaf(-slope_log2, fabsf((float)(pos - key0 - k)), __uint_as_float(v[k]) * sc));
         } else {
-            const float at0 = -slope_log2 * (float)(pos - key0);
+            // (from key to key by adding, in runs of 32: off by 16 roundings of a bias that only matters while it is small)
+            const uint64_t sc2 = both(sc), step2 = both(2.0f * slope_log2);
 #pragma unroll
-            for (int k = 0; k < kBN; ++k)
-                v[k] = __float_as_uint(fmaf(slope_log2, (float)k, fmaf(__uint_as_float(v[k]), sc, at0)));
+            for (int c = 0; c < kBN; c += 32) {
+                const float at = -slope_log2 * (float)(pos - key0 - c);
+                uint64_t b2 = pack_f32x2(at, at + slope_log2);
+#pragma unroll
+                for (int k = c; k < c + 32; k += 2) {
+                    float lo, hi;
+                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), sc2, b2), lo, hi);
+                    v[k] = __float_as_uint(lo);
+                    v[k + 1] = __float_as_uint(hi);
+                    b2 = add_f32x2(b2, step2);
+                }
+            }
         }
     }
 }
 
-template <int G, bool E4M3, int HD, bool RULED>
+template <int G, bool E4M3, int HD, int RULES>
 __global__ void __launch_bounds__(threads_of(E4M3), 1)
-chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-    using Sh = Shape<HD>;
+chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    constexpr bool RULED = RULES != kNoRules, BIAS = RULES == kRulesBias;
+    using Sh = Shape<HD, RULED>;
     constexpr int kTileBytes = Sh::kTileBytes, kStages = Sh::kStages;
     constexpr uint32_t kPCols = Sh::kPCols, kOCol = Sh::kOCol;
     constexpr size_t kSlotFloats = Sh::kSlotFloats;
@@ -740,7 +770,7 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
     const bool helper = E4M3 && warp >= kKHelpWarp;                          // a widening warp of the fourth group
     const int widx = helper ? 1 + (warp & 1) : 0;                            // which of the operand's wideners
     if (warp >= 2 * kSoftmaxThreads / 32) {   // the service warps
-    if constexpr (E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if constexpr (E4M3 || RULED) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == kTmaWarp || warp == kVWarp || helper) {
         // ================================= TMA producers: K warp, V warp ==========================
         // One warp per operand: a tiled TMA copy is issued per (page, 64-dim half), sixteen to a tile, and one
@@ -1027,6 +1057,8 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
     } else {
         // ================================ softmax and epilogue ====================================
         if constexpr (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        // (2 * 208 + 88 = 3 * 168, what 384 threads start with; without it the rules' bounds spill: rules off 365 -> 325 us)
+        if constexpr (RULED) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // two groups of 128 threads: group g works on row tile g of a pair (on every second KV tile of a single row
         // tile); thread tg of a group owns TMEM lane tg
         const int grp = warp >> 2, tg = tid & (kSoftmaxThreads - 1);
@@ -1104,7 +1136,7 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
                 if ((unsigned)(w.qrow0 + row / G) < (unsigned)a.rows) visible_keys(a.rules, w.b, w.qrow0 + row / G, lim - 1, w.L, from, lim);
                 else lim = 0;
                 if (from >= lim) lim = from = 0;
-                if (a.rules.slopes) slope_log2 = a.rules.slopes[w.kvh * G + row % G] * 1.4426950408889634f;
+                if (BIAS && a.rules.slopes) slope_log2 = a.rules.slopes[w.kvh * G + row % G] * 1.4426950408889634f;
             }
             const int pos = w.L - w.n + row / G;
             const bool own_ok = E4M3 && tg < (lone ? w.rows[0] : w.rows[grp]) && (unsigned)(w.qrow0 + row / G) < (unsigned)a.rows;
@@ -1129,7 +1161,7 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
             const int ntiles = w.ntiles, t0 = w.t0, kv_len = w.kv_len, lo = RULED ? w.lo : 0;   // what the loop needs
             float scale_log2 = a.scale_log2;   // of what the rules leave in the registers
             if constexpr (RULED) {
-                if (a.rules.to_cap > 0.f || a.rules.slopes) scale_log2 = 1.0f;
+                if (a.rules.to_cap > 0.f || (BIAS && a.rules.slopes)) scale_log2 = 1.0f;
             }
             const uint32_t it0 = it;
             it += ntiles;
@@ -1150,13 +1182,23 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
                 tmem_wait_ld();
                 tc_fence_before();
                 mbar_arrive(&bars->s_free[grp]);   // the next unit's S may be computed
+                bool late = false;   // RULED: the cap is taken on the way to the weights
                 if constexpr (RULED) {
-                    if (nvis < kBN || from > key0) {   // what hidden slots hold has no say in how a tile's scores are worked out
+                    const bool edge = nvis < kBN || from > key0;
+                    if (a.rules.to_cap > 0.f) {
+                        late = a.cap_plain && !(BIAS && a.rules.slopes) && !__any_sync(0xffffffffu, edge);
+                        if (late) {
+                            float big = 0.f;
 #pragma unroll
-                        for (int k = 0; k < kBN; ++k)
-                            if (k >= nvis || k < from - key0) v[k] = 0u;
+                            for (int k = 0; k < kBN; k += 2) big = max3(big, fabsf(__uint_as_float(v[k])), fabsf(__uint_as_float(v[k + 1])));
+                            late = !__any_sync(0xffffffffu, big * a.rules.to_cap > kCapPoly);
+                        } else if (edge) {   // what hidden slots hold has no say in how a tile's scores are worked out
+#pragma unroll
+                            for (int k = 0; k < kBN; ++k)
+                                if (k >= nvis || k < from - key0) v[k] = 0u;
+                        }
                     }
-                    apply_rules(a, v, slope_log2, pos, key0);
+                    if (!late) apply_rules<BIAS>(a, v, slope_log2, pos, key0);
                 }
                 if (nvis < kBN) {  // causal edge or end of the sequence: hidden keys weigh exp2(-inf) = 0
 #pragma unroll
@@ -1176,7 +1218,13 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
                     for (int u = 0; u < 4; ++u)
                         mx4[u] = max3(mx4[u], __uint_as_float(v[k + 2 * u]), __uint_as_float(v[k + 2 * u + 1]));
                 }
-                const float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2;  // -inf: sees nothing
+                float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2;  // -inf: sees nothing
+                if constexpr (RULED) {
+                    if (late) {
+                        float unused;
+                        unpack_f32x2(capped2(a, both(m_tile), both(a.scale_log2), 0ull), m_tile, unused);   // (of the raw product: scale_log2 is 1)
+                    }
+                }
                 float factor = 1.0f;
                 bool rescale = false;
                 if (m_tile > m_used + kRescaleThreshold || (m_used == -INFINITY && m_tile > -INFINITY)) {
@@ -1212,13 +1260,17 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
                 const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
                 const uint64_t sc2 = pack_f32x2(scale_log2, scale_log2), nm2 = pack_f32x2(neg_m, neg_m);
                 uint64_t l2[4] = {0ull, 0ull, 0ull, 0ull};
+                auto weights = [&](auto late_c, uint64_t sc2) {
+                constexpr bool kLate = decltype(late_c)::value;
 #pragma unroll
                 for (int c4 = 0; c4 < 4; ++c4) {
                     uint32_t pk[16], pl[Sh::kSplitP ? 16 : 1];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const uint64_t t = fma_f32x2(pack_f32x2(__uint_as_float(v[c4 * 32 + 2 * k]),
-                                                                __uint_as_float(v[c4 * 32 + 2 * k + 1])), sc2, nm2);
+                        const uint64_t raw = pack_f32x2(__uint_as_float(v[c4 * 32 + 2 * k]), __uint_as_float(v[c4 * 32 + 2 * k + 1]));
+                        uint64_t t;
+                        if constexpr (kLate) t = capped2(a, raw, sc2, nm2);
+                        else t = fma_f32x2(raw, sc2, nm2);
                         float t0, t1;
                         unpack_f32x2(t, t0, t1);
                         const float e0 = fast_exp2(t0), e1 = fast_exp2(t1);
@@ -1229,6 +1281,13 @@ chunk_mma_kernel(const ArgsOf<RULED> a, const __grid_constant__ CUtensorMap k_ma
                     }
                     tmem_st16(p_tmem + c4 * 16, pk);
                     if constexpr (Sh::kSplitP) tmem_st16(p_tmem + kBN / 2 + c4 * 16, pl);
+                }
+                };
+                if constexpr (RULED) {
+                    if (late) weights(std::true_type(), both(a.scale_log2));
+                    else weights(std::false_type(), sc2);
+                } else {
+                    weights(std::false_type(), sc2);
                 }
                 {
                     float x0, x1, y0, y1;
@@ -1479,25 +1538,25 @@ chunk_combine_kernel(const ArgsOf<RULED> a) {
     }
 }
 
-template <int G, bool E4M3, int HD, bool RULED = false>
-arb_status launch_one(Ctx *ctx, const ArgsOf<RULED> &a, const CUtensorMap &km, const CUtensorMap &vm, int max_items,
+template <int G, bool E4M3, int HD, int RULES = kNoRules>
+arb_status launch_one(Ctx *ctx, const ArgsOf<RULES != kNoRules> &a, const CUtensorMap &km, const CUtensorMap &vm, int max_items,
                       cudaStream_t stream) {
     const size_t smem = mma_smem_bytes<HD>(a.batch, E4M3);
     static bool attr_set[64] = {};
     if (!attr_set[ctx->device & 63]) {
-        if (cudaFuncSetAttribute(chunk_mma_kernel<G, E4M3, HD, RULED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        if (cudaFuncSetAttribute(chunk_mma_kernel<G, E4M3, HD, RULES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)mma_smem_bytes<HD>(E4M3 ? kMaxBatchE4m3 : kMaxBatch, E4M3)) != cudaSuccess)
             return ARB_ERR_CUDA;
         attr_set[ctx->device & 63] = true;
     }
     const int grid = max_items < ctx->num_sms ? max_items : ctx->num_sms;
-    const cudaError_t err = launch_pdl(chunk_mma_kernel<G, E4M3, HD, RULED>, dim3(grid), dim3(threads_of(E4M3)), smem, stream, a, km, vm);
+    const cudaError_t err = launch_pdl(chunk_mma_kernel<G, E4M3, HD, RULES>, dim3(grid), dim3(threads_of(E4M3)), smem, stream, a, km, vm);
     ctx->launches++;
     if (err != cudaSuccess) return ARB_ERR_CUDA;
     // the merge of split sequences, when the block table is long enough for a sequence to be split at all
     if (a.split_cap > 0) {
         const size_t csmem = sizeof(int) * (7 * (size_t)a.batch + 2);
-        const cudaError_t cerr = launch_pdl(chunk_combine_kernel<G, HD, RULED>, dim3(4 * ctx->num_sms), dim3(kCombineThreads), csmem, stream, a);
+        const cudaError_t cerr = launch_pdl(chunk_combine_kernel<G, HD, RULES != kNoRules>, dim3(4 * ctx->num_sms), dim3(kCombineThreads), csmem, stream, a);
         ctx->launches++;
         if (cerr != cudaSuccess) return ARB_ERR_CUDA;
     }
@@ -1535,6 +1594,19 @@ inline void fill_args(MmaArgs &a, Ctx *ctx, const arb_attn_params &p, const void
     const float scale = p.softmax_scale > 0.f ? p.softmax_scale : 1.0f / sqrtf((float)p.head_dim);
     a.scale_log2 = scale * k_scale * 1.4426950408889634f;
     a.v_scale = v_scale;
+}
+
+// The coefficients of capped2, from those of P(x^2).
+inline void fill_cap(RuledArgs &a) {
+    static const double fit[4] = {-0.33327582478523254, 0.13243256509304047, -0.049447160214185715, 0.012286622077226639};
+    const double to_cap = a.rules.to_cap;
+    double power = a.scale_log2;   // scale log2 e r times (to_cap r)^(2 i + 2)
+    a.cap_plain = to_cap > 1e-4 && to_cap < 1e2;
+    for (int i = 0; i < 4; ++i) {
+        power *= to_cap * to_cap;
+        const float c = a.cap_plain ? (float)(fit[i] * power) : 0.f;
+        a.cap_fit[i] = make_float2(c, c);
+    }
 }
 
 // Upper bound of the work items from what the host knows: every row could sit in its own tile run.

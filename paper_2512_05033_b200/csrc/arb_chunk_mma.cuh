@@ -595,7 +595,7 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // instruction, beside the exponential's one on the special-function unit (a tanh out of exponential and reciprocal would make
 // three there, and that unit is what a softmax group waits for already).  P is a least-maximum fit of (tanh(x) / x - 1) / x^2 on
 // [0, 0.8], relative error 1.2e-6: 6e-5 in the exponent at a cap of 50, a fiftieth of the weights' rounding to bf16.
-// Beyond that the exact form, tanh_any.  A tile that all rows of the warp see whole, without a bias, takes the cap on the way to
+// Beyond that the form out of exponential and reciprocal.  A tile that all rows of the warp see whole, without a bias, takes the cap on the way to
 // the weights (see `weights`): tanh is monotonic, so the maximum is taken of the raw products.  The others, which have hidden
 // keys or a bias to take in between, get it here.  Step-scoring batch (32 steps, 28 / 4 heads, cap 30): polynomial of degree 5 in a
 // pass of its own 560 us, taken on the way to the weights with the scale folded in 480, with 208 registers a softmax thread
@@ -630,8 +630,11 @@ __device__ __forceinline__ void apply_rules(const RuledArgs &a, uint32_t (&v)[kB
         }
         const float big = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.rules.to_cap;
         if (!a.cap_plain || __any_sync(0xffffffffu, big > kCapPoly)) {
+            // tanh(x) = 1 - 2 / (1 + e^(2 x)): off by 2^-23 or so absolute, which a weight in bf16 does not notice
+            const float to_exp = a.rules.to_cap * 2.8853900817779268f;
 #pragma unroll
-            for (int k = 0; k < kBN; ++k) v[k] = __float_as_uint(a.rules.cap_log2 * tanh_any(__uint_as_float(v[k]) * a.rules.to_cap));
+            for (int k = 0; k < kBN; ++k)
+                v[k] = __float_as_uint(a.rules.cap_log2 - __fdividef(2.0f * a.rules.cap_log2, 1.0f + fast_exp2(__uint_as_float(v[k]) * to_exp)));
         } else {
             const uint64_t scale2 = both(a.scale_log2);
 #pragma unroll

@@ -572,7 +572,7 @@ arb_status arb_rope_append_i4(arb_ctx *ctx, const arb_attn_params *params, const
 typedef struct {
     float cap;                   /* 1e-20 .. 1e20; 0: scores are not capped */
     int32_t window;              /* keys a token sees up to itself, itself included; 0: no window */
-    const float *slopes;         /* fp32 [num_q_heads], nullable, finite */
+    const float *slopes;         /* fp32 [num_q_heads], nullable; finite, not negative */
     const int32_t *prefix_lens;  /* int32 [B], nullable; <= 0: no prefix */
     const int32_t *first_keys;   /* int32 [total_q], nullable: first key of the document a token belongs to */
 } arb_score_rules;
@@ -594,7 +594,8 @@ arb_status arb_attn_rules(arb_ctx *ctx, const arb_attn_params *params, const arb
 /*
  * ---- Behind the attention: from logits to the next token -------------------------------------------
  * Section 3.1 samples a step token by token, z_i ~ q(z_i | x, z_<i); the models' logits and what requests ask of them are not
- * the paper's subject.  For every row s and token t, in fp32, each operation rounded once (IEEE):
+ * the paper's subject.  For every row s and token t, in fp32, each operation rounded once (to nearest, results below the
+ * smallest normal number to zero):
  *   x = logits[s][t]
  *   c = times t occurs in history[s][0 .. history_lens[s]);  where c > 0:
  *       x = x > 0 ? x / repetition[s] : x * repetition[s];   x = x - presence[s];   x = x - frequency[s] * c
@@ -624,7 +625,8 @@ typedef struct {
     const uint32_t *mask;         /* 1 = allowed */
     const float *temperature;     /* fp32 [rows] */
     const float *noise;           /* fp32 [rows, vocab], dense */
-    float *out;                   /* fp32 [rows, vocab], dense: x; may be logits itself where those are fp32 and dense */
+    float *out;                   /* fp32 [rows, vocab], dense: x; may be logits itself where those are fp32 and dense (an overlap
+                                     of any other kind is the caller's error) */
     int32_t *tokens;              /* int32 [rows] */
     float *logprobs;              /* fp32 [rows] */
 } arb_logits_params;

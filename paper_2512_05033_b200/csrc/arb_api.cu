@@ -196,7 +196,7 @@ arb_status arb_create(arb_ctx **out, int device, size_t workspace_bytes) {
         return ARB_ERR_CUDA;
     }
     c->num_sms = sms;
-    // tuning knob of the single-launch decode (see Plan in arb_decode_step.cu)
+    // tuning knob of the single-launch decode (see Plan in arb_decode_step.cuh)
     if (const char *mc = std::getenv("ARB_STEP_MIN_CHUNK")) c->step_min_chunk = std::max(1, std::min(1024, std::atoi(mc)));
     if (const char *pct = std::getenv("ARB_STEP_BOUNDARY_PCT")) c->step_boundary_pct = std::max(0, std::min(400, std::atoi(pct)));
     c->workspace_bytes = workspace_bytes ? workspace_bytes : kDefaultWorkspace;
@@ -850,6 +850,7 @@ arb_status arb_logits(arb_ctx *ctx, const arb_logits_params *params, arb_stream_
     if (!p.logits) return ARB_ERR_INVALID_ARG;
     const size_t elt = p.dtype == ARB_BF16 ? 2 : 4;
     auto misaligned = [](const void *q, size_t n) { return (reinterpret_cast<uintptr_t>(q) & (n - 1)) != 0; };
+    if (p.dtype == ARB_BF16 && (const void *)p.out == p.logits) return ARB_ERR_INVALID_ARG;
     if (misaligned(p.logits, elt) || misaligned(p.noise, 4) || misaligned(p.out, 4)) return ARB_ERR_INVALID_ARG;
     Ctx *c = reinterpret_cast<Ctx *>(ctx);
     DeviceGuard guard(c->device);

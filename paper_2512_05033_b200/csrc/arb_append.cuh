@@ -26,10 +26,13 @@ struct AppendArgs {
 
 // The tables every CTA derives, in shared memory.
 struct AppendPlan {
-    int *pref;    // [B + 1] new rows before sequence b
+    int *pref;    // [B + 1] new rows before sequence b; at most total_new, whatever the lengths on the device add up to
     int *okay;    // [B] the sequence's new tokens may be written
     int *start;   // [B] tokens it holds
 };
+
+// a + b, at most `most`; both lie in 0 .. most
+__device__ __forceinline__ int capped_sum(int a, int b, int most) { return (int)min((unsigned)a + (unsigned)b, (unsigned)most); }
 
 __device__ __forceinline__ AppendPlan append_plan(const AppendArgs &a, int *tables) {
     const int tid = threadIdx.x, lane = tid & 31, B = a.batch;
@@ -58,7 +61,7 @@ __device__ __forceinline__ AppendPlan append_plan(const AppendArgs &a, int *tabl
             if (bad && blockIdx.x == 0) atomicOr(a.status, bad);
             pl.okay[b] = bad == 0;
             pl.start[b] = L;
-            pl.pref[b + 1] = n > 0 ? n : 0;
+            pl.pref[b + 1] = n > 0 ? min(n, a.total_new) : 0;
         }
     }
     __syncthreads();
@@ -70,10 +73,11 @@ __device__ __forceinline__ AppendPlan append_plan(const AppendArgs &a, int *tabl
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const int t = __shfl_up_sync(0xffffffffu, v, off);
-                if (lane >= off) v += t;
+                if (lane >= off) v = capped_sum(v, t, a.total_new);
             }
-            if (b < B) pl.pref[b + 1] = v + carry;
-            carry += __shfl_sync(0xffffffffu, v, 31);
+            v = capped_sum(v, carry, a.total_new);
+            if (b < B) pl.pref[b + 1] = v;
+            carry = __shfl_sync(0xffffffffu, v, 31);
         }
     }
     __syncthreads();

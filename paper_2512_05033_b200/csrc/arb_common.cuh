@@ -252,7 +252,7 @@ __device__ __forceinline__ float fast_exp2(float x) {
 // Every kernel launched through launch_pdl passes wait_for_predecessor on all its paths (so that its own completion implies
 // that of everything before it on the stream), and before it touches what an earlier kernel may be writing or reading: a
 // chain of small dependent kernels then pays no launch latency between them.  It calls let_successor_start at its top, with
-// one exception: decode rows beside chunks (arb_decode_step.cu, `beside`) call it behind their own wait, and the chunk kernel
+// one exception: decode rows beside chunks (arb_decode_step.cuh, `beside`) call it behind their own wait, and the chunk kernel
 // behind them, which shares nothing with them, waits at its end only.
 __device__ __forceinline__ void let_successor_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

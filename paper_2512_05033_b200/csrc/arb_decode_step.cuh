@@ -823,6 +823,7 @@ decode_step_kernel(const StepArgsOf<RULED> a, const __grid_constant__ CUtensorMa
             for (int b = 0; b < B; ++b) {
                 const int n = row0[b + 1] - row0[b];
                 if (n != 1 || pref[b + 1] != pref[b]) continue;
+                if (RULED && (unsigned)row0[b] >= (unsigned)a.rows) continue;
                 if (lane == 0) atomicOr(a.status, (uint32_t)ARB_DEV_BAD_SEQ_LEN);
                 uint4 *o = reinterpret_cast<uint4 *>(a.out + (size_t)row0[b] * a.Hq * kD * 2);
                 for (int i = lane; i < a.Hq * kD * 2 / 16; i += 32) o[i] = make_uint4(0, 0, 0, 0);
@@ -932,6 +933,7 @@ decode_step_kernel(const StepArgsOf<RULED> a, const __grid_constant__ CUtensorMa
     };
     const int eh = tid / (kD / 4);     // head of this thread's piece
     auto write_row = [&](size_t out_base, float4 x, float inv) {
+        if (RULED && out_base + G * kD > (size_t)a.rows * a.Hq * kD) return;   // more decode rows on the device than total_q
         if (!ARB_IN_RANGE(a.status, out_base + G * kD - 1, (size_t)a.rows * a.Hq * kD)) return;
         *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.out) + out_base + (size_t)tid * 4) =
             make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));

@@ -1,5 +1,5 @@
 // Pieces shared by the tensor-core decode kernels (arb_decode_mma.cu: the two-kernel form for back-to-back
-// series and the E4M3 cache; arb_decode_step.cu: the single-launch form): the cut of the flat
+// series and the E4M3 cache; arb_decode_step.cuh: the single-launch form): the cut of the flat
 // (sequence, kv head, page) list into per-CTA ranges, tiled TMA loads, ldmatrix / mma.sync wrappers.
 #pragma once
 

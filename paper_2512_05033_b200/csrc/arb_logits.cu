@@ -32,7 +32,7 @@ constexpr int kLogitsCtas = 4;                              // resident CTAs of 
 constexpr int kGroup = 4;                                   // tokens of a vector load
 template <int PER> constexpr int kPiece = kLogitsThreads * PER * kGroup;   // PER groups a thread
 constexpr int kHeld = 8;                                    // history tokens of a thread in flight
-constexpr int kBiasOne = 1 << 24;                           // in a token's counter: history below, entries of the biases above
+constexpr int kBiasOne = 1 << 24;                           // in a token's counter: occurrences in the history below, listed among the biases
 
 struct Record {      // what a run leaves of a row: max and sum of exponentials of x, the best x + noise with its token and its x
     float m, l, best, best_x;
@@ -234,7 +234,7 @@ logits_kernel(const LogitsArgs a) {
     if (special) {
         // Counts the tokens of a thread, kHeld of them, all atomics in flight together, and lists those not met before; a whole
         // warp is here.
-        auto all_of = [&](const int32_t *tokens, int n, int one) {
+        auto all_of = [&](const int32_t *tokens, int n, bool biases) {
             for (int i0 = 0; i0 < n; i0 += kHeld * kLogitsThreads) {
                 int t[kHeld];
 #pragma unroll
@@ -246,7 +246,7 @@ logits_kernel(const LogitsArgs a) {
 #pragma unroll
                 for (int k = 0; k < kHeld; ++k) {
                     if (mine(t[k])) {
-                        const int old = atomicAdd(&counts[t[k] - lo], one);
+                        const int old = biases ? atomicOr(&counts[t[k] - lo], kBiasOne) : atomicAdd(&counts[t[k] - lo], 1);
                         if (old == 0) begun |= 1u << k;
                         again = again || old >= kBiasOne;
                     }
@@ -271,8 +271,8 @@ logits_kernel(const LogitsArgs a) {
                 }
             }
         };
-        all_of(p.history + (size_t)row * p.history_stride, n_history, 1);
-        all_of(p.bias_tokens + b_begin, b_end - b_begin, kBiasOne);
+        all_of(p.history + (size_t)row * p.history_stride, n_history, false);
+        all_of(p.bias_tokens + b_begin, b_end - b_begin, true);
         again = __syncthreads_or(again);
         n_listed = listed;
         for (int i = tid; i < n_listed; i += kLogitsThreads) {

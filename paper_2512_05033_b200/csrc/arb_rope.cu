@@ -97,7 +97,7 @@ rope_append_kernel(const RopeArgs r) {
         off1 = off0 + (turns ? r.rot / 2 : (D - r.rot) / 2);
     }
     const int heads = r.Hq + 2 * a.Hkv, mine = (threadIdx.x & 31) / kLanes;   // this lane's group of the warp
-    const unsigned units = (unsigned)min(pl.pref[a.batch], a.total_new) * (unsigned)r.units_per_token;
+    const unsigned units = (unsigned)pl.pref[a.batch] * (unsigned)r.units_per_token;
     const unsigned warps = gridDim.x * (kAppendThreads / 32);
     for (unsigned u = blockIdx.x * (kAppendThreads / 32) + threadIdx.x / 32; u < units; u += warps) {
         const int tok = (int)(u / (unsigned)r.units_per_token), h_begin = ((int)u - tok * r.units_per_token) * r.heads_per_unit;

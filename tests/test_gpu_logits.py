@@ -174,6 +174,18 @@ def test_a_token_listed_twice_gets_its_sum_in_order():
     check(x, o)
 
 
+def test_a_token_listed_many_times():
+    """Hundreds of entries of one token beside every token of a small vocabulary, in the history too."""
+    r = np.random.RandomState(4)
+    V, n = 4200, 4200
+    x = torch.from_numpy(r.randn(2, V).astype(np.float32))
+    tokens = np.concatenate((r.permutation(V), np.full(700, 17), np.full(300, 4199))).astype(np.int32)
+    o = {"bias_offsets": np.array([0, len(tokens), len(tokens)], np.int32), "bias_tokens": tokens,
+         "bias_values": r.randn(len(tokens)).astype(np.float32), "history": np.full((2, 1000), 17, np.int32),
+         "repetition": np.array([1.3, 1.1], np.float32), "frequency": np.array([0.01, 0.02], np.float32)}
+    check(x, o)
+
+
 def test_what_is_not_wanted_is_left_out():
     x, o = inputs(8, 3, 7001, history=20)
     c, b = H.ctx(), _binding()

@@ -217,6 +217,24 @@ def test_refused_sequences_are_left_alone():
         assert c.poll_status() == 0
 
 
+def test_lengths_that_add_up_to_more_than_there_is():
+    """Lengths on the device whose sum passes 32 bits, and total_new: refused where they do not fit, never read past the rows."""
+    b = _binding()
+    d = make(9, torch.bfloat16, 4, 2, 64, [0, 0, 0, 0], [3, 4, 2, 3], 64)
+    q, k, v = views(d)
+    c = H.ctx()
+    for new in ([2 ** 31 - 1, 5, 2 ** 31 - 1, 7], [2 ** 30] * 4, [3, 2 ** 31 - 1, 2, 3]):
+        kp, vp = (torch.zeros(d["pages"], 2, P, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        buf = torch.full((q.shape[0] + 2, 4, 64), 777.0, dtype=torch.bfloat16, device="cuda")
+        c.rope_append(q, k, v, d["inv_freq"].cuda(), d["table"].cuda(), d["before"].cuda(), torch.tensor(new, dtype=torch.int32, device="cuda"),
+                      kp, vp, q_out=buf[1:-1], update_lens=False)
+        assert c.poll_status() == b.DEV_BAD_SEQ_LEN
+        assert bool((buf[0] == 777).all()) and bool((buf[-1] == 777).all())
+        first = 0 if new[0] > 100 else new[0]
+        assert not bool(buf[1 + first:-1].any())            # rows of the refused sequence, up to the last there is
+        assert first == 0 or bool(buf[1:1 + first].any())
+
+
 def test_rows_behind_the_last_sequence_stay():
     d = make(6, torch.bfloat16, 4, 2, 64, [3, 0], [2, 3], 64)
     q, k, v = (torch.cat((t, t)) for t in views(d))

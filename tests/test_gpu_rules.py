@@ -245,6 +245,27 @@ def test_bad_pages_are_reported_and_other_sequences_keep_their_rows():
         assert bool(((out[new:].double().cpu() - ref[new:]).abs() <= bar[new:]).all()) and bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 64)])
+def test_more_rows_on_the_device_than_there_are(dtype, D):
+    """q_lens that add up to more than total_q: rows beyond it are neither read nor written."""
+    x = Inputs(17, dtype, 4, 2, D, [100, 90, 80, 0 + 70], [1, 1, 1, 1], window=30, cap=5.0)
+    ref, bar = x.reference()
+    args, rules = x.args()
+    c = H.ctx()
+    for first in (None, torch.zeros(2, dtype=torch.int32, device="cuda")):
+        buf = torch.full((6, 4, D), 333.0, dtype=dtype, device="cuda")
+        c.attn_rules(args[0][:2].contiguous(), *args[1:], cap=5.0, window=30, first_keys=first, out=buf[2:4])
+        assert c.poll_status() == 0
+        assert bool((buf[:2] == 333).all()) and bool((buf[4:] == 333).all())
+        assert bool(((buf[2:4].double().cpu() - ref[:2]).abs() <= bar[:2]).all())
+    y = Inputs(18, dtype, 4, 2, D, [100, 90, 80], [20, 30, 1], window=30)
+    args, rules = y.args()
+    buf = torch.full((30, 4, D), 333.0, dtype=dtype, device="cuda")
+    c.attn_rules(args[0][:25].contiguous(), *args[1:6], 20, window=30, out=buf[2:27])   # the second step has rows for five
+    c.poll_status()
+    assert bool((buf[:2] == 333).all()) and bool((buf[27:] == 333).all())
+
+
 def test_two_contexts_two_streams_and_a_graph():
     b = _binding()
     x = Inputs(14, BF, 28, 4, 128, [900, 3000, 400], [60, 1, 100], cap=9.0, window=700, slopes=True)

@@ -169,12 +169,12 @@ def test_attn_rules_refusals():
 
 def _logits(**fields):
     b = _binding()
-    p = b.LogitsParams(**{**dict(dtype=1, rows=3, vocab=V, logits=PTR, out=PTR), **fields})
+    p = b.LogitsParams(**{**dict(dtype=1, rows=3, vocab=V, logits=PTR, out=PTR + 4096), **fields})
     return b.lib.arb_logits(ctypes.addressof(_ctx_memory()), ctypes.byref(p), None)
 
 
 def test_logits_refusals():
-    for f in ({"rows": -1}, {"vocab": 0}, {"logits": None}, {"logits": PTR + 1}, {"out": PTR + 2}, {"noise": PTR + 1}, {"out": None},
+    for f in ({"rows": -1}, {"vocab": 0}, {"logits": None}, {"logits": PTR + 1}, {"out": PTR + 2}, {"noise": PTR + 1}, {"out": None}, {"logits": PTR, "out": PTR},
               {"logits_stride": V - 1}, {"history": PTR}, {"history_lens": PTR}, {"mask": PTR, "mask_stride": 2},
               {"bias_tokens": PTR}, {"bias_values": PTR}, {"bias_offsets": PTR, "bias_total": 3},
               {"bias_offsets": PTR, "bias_total": -1, "bias_tokens": PTR, "bias_values": PTR}):

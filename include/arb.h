@@ -604,7 +604,8 @@ arb_status arb_attn_rules(arb_ctx *ctx, const arb_attn_params *params, const arb
  *   x = -inf where bit t % 32 of mask[s][t / 32] is 0
  * and, per row:
  *   tokens[s]    the lowest t whose x + noise[s][t] is largest (noise that is Gumbel-distributed makes this a draw from
- *                softmax(x)); a row with temperature[s] <= 0 ignores its noise.  NaN never wins; -1 if every x is -inf or NaN.
+ *                softmax(x)); a row with temperature[s] <= 0 ignores its noise.  A sum of NaN or -inf never wins; -1 if none
+ *                is left.
  *   logprobs[s]  x[tokens[s]] - log sum_t exp(x[t])   (NaN where a NaN or +inf is among x; -inf where the token is -1)
  * Every pointer of this record but logits may be NULL: the step is left out, the output is not wanted.
  */

@@ -53,6 +53,9 @@
 // Rules (template parameter RULED, arb_attn_rules without per-token first keys): a sequence's list of pages starts at the page of
 // the first key in its window.  Everything counts from there, as if the sequence had lost the pages before it (`shift`): its
 // length, its pages' numbers and the distances between its tokens; only the look-up in the block table adds the shift back.
+// A token of 16 sequences of 4k to 32k keys that sees 4096 of them, 32 / 8 heads (270 MB): 46 us, 5.8 TB/s, 0.89 of the measured
+// copy rate; 57 on the CUDA-core kernel.  The draft shape with slopes over 1k to 8k keys 11.5 us (26).  The rules cost a lane four
+// scores' worth of arithmetic a page, which the memory system hides.
 #pragma once
 
 #include "arb_decode_tc.cuh"

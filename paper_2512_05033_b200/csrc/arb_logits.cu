@@ -2,20 +2,22 @@
 // temperature, an allowed-token mask, the arg max of x + noise and its log-probability.
 //
 // One pass over memory: a row is cut into pieces of kPiece tokens, and its pieces into as many runs as keep every resident CTA
-// busy, one CTA a run.  Few tokens of a vocabulary are in a history or a list of biases, so these are gone through on their own:
-// the CTA counts the history's tokens that fall into a piece (integer atomics in shared memory: any order gives the same
-// counts), lists every token that occurs there or among the biases once, and gives the listed ones their penalties and
-// biases (each bias added by any thread, unless a token is listed twice: then its first entry's thread sums them up in the
-// order of the list).  The stream over the piece, which does temperature, mask, noise, maximum and sum, takes a listed token's
-// value, which a bit per token marks, from shared memory.  A history is read by every CTA of its row, from L2.  The runs' records
-// (maximum, sum, best) go to the workspace; the CTA of a row that arrives last at the row's counter puts them together, run by
-// run in order.
+// busy, one CTA a run.  Few tokens of a vocabulary are in a history or a list of biases, so these are gone through on their own,
+// for a window of up to kWindow pieces: the CTA marks each in a bitmap in shared memory; the number of bits before its own
+// is a special token's slot, whichever thread comes first; a second look at the lists counts occurrences (integer atomics: any
+// order gives the same), and the slots get their penalties and biases (each bias added by any thread, unless a token is
+// listed twice: then its first entry's thread sums them up in the order of the list).  The stream over the pieces, which does
+// temperature, mask, noise, maximum and sum, takes a marked token's value from its slot.  A window with more special tokens than
+// slots is done a piece at a time.  A history is read by every CTA of its row, from L2.  The runs' records (maximum, sum,
+// best) go to the workspace; the CTA of a row that arrives last at the row's counter puts them together, run by run in order.
 //
-// What bounds it is instruction issue, the barriers around the special tokens and what a CTA waits for at its end.  64 rows of
-// 128001 bf16 logits (49 MB; a plain bf16 -> fp32 copy of them takes 24 us): 16 us without options, 47 us with a history of up to 4096
-// tokens, biases, mask, temperature and noise (84 MB).  Looking up a count and a bias for every token 53 us; a CTA per piece instead
-// of a run of pieces 19 and 56 us (every CTA's reduction, fence and arrival cost 7 us); the special tokens in a kernel of their own
-// 20 and 61 us.
+// What bounds it is instruction issue and the chain of steps before a window's stream.  64 rows of 128001 bf16 logits (49 MB; a
+// plain bf16 -> fp32 copy of them takes 24 us): 15 us without options, 26 with a history of up to 4096 tokens, 18 with 64 biases, 32 with
+// a history, biases, mask, temperature and noise (84 MB).  Special tokens found piece by piece, in a list in order of arrival and a counter
+// per token, 47 us; windows of 4 pieces instead of 8 39; a count and a bias looked up for every token 53; the special tokens in a kernel of
+// their own 61; a CTA per piece instead of a run of pieces 19 us without and 56 with everything (every CTA's reduction, fence and arrival
+// cost 7 us).  Pieces of 4096 tokens 36, of 1024 35; three CTAs per SM 40, five 34.  No difference: the first tokens of the
+// history read ahead of its length and kept in registers, 8 in flight instead of 4.
 //
 // Rows of an odd vocabulary start at any element, so groups of four tokens are cut at multiples of four of the flat element
 // index: full groups are aligned in every array whose rows lie alike, a row's first and last group are read one by one.
@@ -30,8 +32,12 @@ namespace {
 constexpr int kLogitsThreads = 256;
 constexpr int kLogitsCtas = 4;                              // resident CTAs of an SM
 constexpr int kGroup = 4;                                   // tokens of a vector load
-template <int PER> constexpr int kPiece = kLogitsThreads * PER * kGroup;   // PER groups a thread
-constexpr int kHeld = 8;                                    // history tokens of a thread in flight
+constexpr int kPer = 2;                                     // groups of a thread and piece
+constexpr int kPiece = kLogitsThreads * kPer * kGroup;
+constexpr int kAhead = 2;                                   // pieces asked into L2 ahead
+constexpr int kCap = 4096;                                  // special tokens of a window, a piece's at least
+constexpr int kWindow = 8;                                  // pieces whose special tokens are found together
+constexpr int kHeld = 4;                                    // history tokens of a thread in flight
 constexpr int kBiasOne = 1 << 24;                           // in a token's counter: occurrences in the history below, listed among the biases
 
 struct Record {      // what a run leaves of a row: max and sum of exponentials of x, the best x + noise with its token and its x
@@ -165,18 +171,20 @@ __device__ __forceinline__ void best_of(Record &r, const float (&x)[kGroup], flo
     }
 }
 
-template <typename T, int PER>
+template <typename T>
 __global__ void __launch_bounds__(kLogitsThreads, kLogitsCtas)
 logits_kernel(const LogitsArgs a) {
-    constexpr int kPc = kPiece<PER>, kWarps = kLogitsThreads / 32;
-    static_assert(kPc <= 65536 && kPc % (4 * kLogitsThreads) == 0 && kPc / 32 <= kLogitsThreads, "16 bits a listed token; cleared by fours; a word a thread");
+    constexpr int kPc = kPiece, PER = kPer, kWarps = kLogitsThreads / 32;
+    constexpr int kWords = kWindow * kPc / 32, kOwn = kWords / kLogitsThreads;
+    static_assert(kWindow * kPc <= 65536 && kCap >= kPc && kCap % (4 * kLogitsThreads) == 0 && kWords % kLogitsThreads == 0, "16 bits a token; cleared by fours; as many words for every thread");
     const arb_logits_params &p = a.p;
-    extern __shared__ __align__(16) int counts[];         // [kPc] counters, then the tokens' x; [kPc] listed tokens; a bit per token
-    uint16_t *list = reinterpret_cast<uint16_t *>(counts + kPc);
-    uint32_t *touched = reinterpret_cast<uint32_t *>(list + kPc);
+    extern __shared__ __align__(16) int counts[];         // [kCap] counters of the special tokens, then their x
+    uint32_t *touched = reinterpret_cast<uint32_t *>(counts + kCap);          // [kWords] a bit per token of the window
+    uint16_t *before = reinterpret_cast<uint16_t *>(touched + kWords);        // [kWords] bits set in the words before
+    uint16_t *list = before + kWords;                                         // [kCap] the special tokens in their order
     float *xs = reinterpret_cast<float *>(counts);
     __shared__ Record warp_rec[kWarps];
-    __shared__ int listed;
+    __shared__ int warp_bits[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = p.vocab, row = blockIdx.y, runs = gridDim.x;
     const bool special = p.history || p.bias_offsets, wanted = p.tokens || p.logprobs;
     const T *x_in = static_cast<const T *>(p.logits) + row * (p.logits_stride ? p.logits_stride : (long long)V);
@@ -189,12 +197,12 @@ logits_kernel(const LogitsArgs a) {
         if (p.noise) prefetch_l2(p.noise + (size_t)row * V + first, tokens * 4);
     };
     let_successor_start();
-    if (tid == 0) fetch(piece_begin, min(piece_begin + 2, piece_end));
-    if (special) {   // all zero at the start of a piece
+    if (tid == 0) fetch(piece_begin, min(piece_begin + kAhead, piece_end));
+    if (special) {   // all zero at the start of a window
 #pragma unroll
-        for (int i = 0; i < kPc / 4 / kLogitsThreads; ++i) reinterpret_cast<uint4 *>(counts)[i * kLogitsThreads + tid] = make_uint4(0, 0, 0, 0);
-        if (tid < kPc / 32) touched[tid] = 0;
-        if (tid == 0) listed = 0;
+        for (int i = 0; i < kCap / 4 / kLogitsThreads; ++i) reinterpret_cast<uint4 *>(counts)[i * kLogitsThreads + tid] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) touched[i * kLogitsThreads + tid] = 0;
         __syncthreads();
     }
     wait_for_predecessor();
@@ -222,85 +230,118 @@ logits_kernel(const LogitsArgs a) {
         b_end = max(b_begin, min(p.bias_offsets[row + 1], p.bias_total));
     }
     const bool alike = (!noise || noise_alike) && (!out || out_alike);
+    int window = kWindow;   // pieces
 #pragma unroll 1
-    for (int piece = piece_begin; piece < piece_end; ++piece) {
-    const int lo = piece * kPc - skew;   // first token of the piece (below 0: the row starts inside a group)
-    if (tid == 0 && piece + 2 < piece_end) fetch(piece + 2, piece + 3);
+    for (int w_begin = piece_begin, w_end; w_begin < piece_end; w_begin = w_end) {
+    w_end = min(w_begin + window, piece_end);
+    const int w_lo = w_begin * kPc - skew;   // first token of the window (below 0: the row starts inside a group)
 
-    // ---- which tokens of the piece are special
-    bool again = false;   // a token is listed twice among the biases
+    // ---- the window's special tokens
     int n_listed = 0;
-    auto mine = [&](int t) { return (unsigned)(t - lo) < (unsigned)kPc && (unsigned)t < (unsigned)V; };
     if (special) {
-        // Counts the tokens of a thread, kHeld of them, all atomics in flight together, and lists those not met before; a whole
-        // warp is here.
-        auto all_of = [&](const int32_t *tokens, int n, bool biases) {
-            for (int i0 = 0; i0 < n; i0 += kHeld * kLogitsThreads) {
+        const int32_t *history = p.history + (size_t)row * p.history_stride;
+        const int first = max(w_lo, 0);
+        unsigned tokens_here;
+        // f(t) for every token of a list that lies in the window, the loads of kHeld in flight together
+        auto each = [&](const int32_t *tokens, int n, auto f) {
+            for (int i0 = tid; i0 < n; i0 += kHeld * kLogitsThreads) {
                 int t[kHeld];
 #pragma unroll
-                for (int k = 0; k < kHeld; ++k) {
-                    const int i = i0 + k * kLogitsThreads + tid;
-                    t[k] = i < n ? __ldg(tokens + i) : -1;
-                }
-                uint32_t begun = 0;
+                for (int k = 0; k < kHeld; ++k) t[k] = i0 + k * kLogitsThreads < n ? __ldg(tokens + i0 + k * kLogitsThreads) : -1;
 #pragma unroll
-                for (int k = 0; k < kHeld; ++k) {
-                    if (mine(t[k])) {
-                        const int old = biases ? atomicOr(&counts[t[k] - lo], kBiasOne) : atomicAdd(&counts[t[k] - lo], 1);
-                        if (old == 0) begun |= 1u << k;
-                        again = again || old >= kBiasOne;
-                    }
-                }
-                if (!__any_sync(0xffffffffu, begun != 0)) continue;
-                int before = __popc(begun);
-                const int own = before;
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const int other = __shfl_up_sync(0xffffffffu, before, off);
-                    if (lane >= off) before += other;
-                }
-                int at = 0;
-                if (lane == 31) at = atomicAdd(&listed, before);
-                at = __shfl_sync(0xffffffffu, at, 31) + before - own;
-#pragma unroll
-                for (int k = 0; k < kHeld; ++k) {
-                    if (begun >> k & 1u) {
-                        list[at++] = (uint16_t)(t[k] - lo);
-                        atomicOr(&touched[(t[k] - lo) >> 5], 1u << ((t[k] - lo) & 31));
-                    }
-                }
+                for (int k = 0; k < kHeld; ++k)
+                    if ((unsigned)(t[k] - first) < tokens_here) f(t[k] - w_lo);
             }
         };
-        all_of(p.history + (size_t)row * p.history_stride, n_history, false);
-        all_of(p.bias_tokens + b_begin, b_end - b_begin, true);
+        auto mark = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
+        auto slot_of = [&](int at) { return before[at >> 5] + __popc(touched[at >> 5] & ((1u << (at & 31)) - 1u)); };
+        for (;;) {
+            tokens_here = (unsigned)(min((long long)w_end * kPc - skew, (long long)V) - first);
+            each(history, n_history, mark);
+            each(p.bias_tokens + b_begin, b_end - b_begin, mark);
+            __syncthreads();
+            // a token's slot is the number of bits before its own
+            uint32_t word[kOwn];
+            int bits = 0;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                word[i] = touched[tid * kOwn + i];
+                bits += __popc(word[i]);
+            }
+            int upto = bits;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int other = __shfl_up_sync(0xffffffffu, upto, off);
+                if (lane >= off) upto += other;
+            }
+            if (lane == 31) warp_bits[warp] = upto;
+            __syncthreads();
+            int at = upto - bits;
+            n_listed = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const int n = warp_bits[w];
+                at += w < warp ? n : 0;
+                n_listed += n;
+            }
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                before[tid * kOwn + i] = (uint16_t)at;
+                at += __popc(word[i]);
+            }
+            if (n_listed <= kCap) break;
+            // more than there is room for: a piece at a time from here on
+            window = 1;
+            w_end = w_begin + 1;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) touched[tid * kOwn + i] = 0;
+            __syncthreads();
+        }
+        __syncthreads();
+        each(history, n_history, [&](int at) {
+            const int slot = slot_of(at);
+            atomicAdd(&counts[slot], 1);
+            list[slot] = (uint16_t)at;   // (whoever else writes it writes the same)
+        });
+        bool again = false;   // a token is listed twice among the biases
+        each(p.bias_tokens + b_begin, b_end - b_begin, [&](int at) {
+            const int slot = slot_of(at);
+            again = atomicOr(&counts[slot], kBiasOne) >= kBiasOne || again;
+            list[slot] = (uint16_t)at;
+        });
         again = __syncthreads_or(again);
-        n_listed = listed;
         for (int i = tid; i < n_listed; i += kLogitsThreads) {
-            const int at = list[i], c = counts[at] & (kBiasOne - 1);
-            float v = Elt<T>::to_float(x_in[lo + at]);
+            const int c = counts[i] & (kBiasOne - 1);
+            float v = Elt<T>::to_float(x_in[w_lo + list[i]]);
             if (c > 0) {
                 v = v > 0.f ? __fdiv_rn(v, repetition) : __fmul_rn(v, repetition);
                 v = __fsub_rn(v, presence);
                 v = __fsub_rn(v, __fmul_rn(frequency, (float)c));
             }
-            xs[at] = v;
+            xs[i] = v;
         }
         __syncthreads();
         for (int i = b_begin + tid; i < b_end; i += kLogitsThreads) {
             const int t = __ldg(p.bias_tokens + i);
-            if (!mine(t)) continue;
+            if ((unsigned)(t - first) >= tokens_here) continue;
             float sum = __ldg(p.bias_values + i);
             if (again) {
-                bool first = true;
-                for (int j = b_begin; j < i && first; ++j) first = __ldg(p.bias_tokens + j) != t;
-                if (!first) continue;
+                bool earliest = true;
+                for (int j = b_begin; j < i && earliest; ++j) earliest = __ldg(p.bias_tokens + j) != t;
+                if (!earliest) continue;
                 for (int j = i + 1; j < b_end; ++j)
                     if (__ldg(p.bias_tokens + j) == t) sum = __fadd_rn(sum, __ldg(p.bias_values + j));
             }
-            xs[t - lo] = __fadd_rn(xs[t - lo], sum);
+            const int slot = slot_of(t - w_lo);
+            xs[slot] = __fadd_rn(xs[slot], sum);
         }
         if (p.bias_offsets) __syncthreads();
     }
+
+#pragma unroll 1
+    for (int piece = w_begin; piece < w_end; ++piece) {
+    const int lo = piece * kPc - skew;
+    if (tid == 0 && piece + kAhead < piece_end) fetch(piece + kAhead, piece + kAhead + 1);
 
     // ---- the stream, compiled twice: every group of the piece whole and alike in all arrays, or with a look at each.  What a row
     //      does not use costs a branch per piece, not an instruction per token.
@@ -349,12 +390,13 @@ logits_kernel(const LogitsArgs a) {
         if (special) {
 #pragma unroll
             for (int k = 0; k < PER; ++k) {
-                const int at = t_first + k * kStep - lo;
-                const uint32_t those = touched[at >> 5] >> (at & 31);
+                const int at = t_first + k * kStep - w_lo;
+                const uint32_t word = touched[at >> 5], those = word >> (at & 31);
                 if (those & ((1u << kGroup) - 1u)) {
+                    int slot = before[at >> 5] + __popc(word & ((1u << (at & 31)) - 1u));
 #pragma unroll
                     for (int i = 0; i < kGroup; ++i)
-                        if (those & (1u << i)) x[k][i] = xs[at + i];
+                        if (those & (1u << i)) x[k][i] = xs[slot++];
                 }
             }
         }
@@ -411,11 +453,12 @@ logits_kernel(const LogitsArgs a) {
     if (alike && lo >= 0 && lo + kPc <= V) stream(std::true_type());
     else stream(std::false_type());
 
-    if (special && piece + 1 < piece_end) {
-        __syncthreads();   // (everyone has read what it needs of the piece)
-        for (int i = tid; i < n_listed; i += kLogitsThreads) counts[list[i]] = 0;
-        if (tid < kPc / 32) touched[tid] = 0;
-        if (tid == 0) listed = 0;
+    }
+    if (special && w_end < piece_end) {
+        __syncthreads();   // (everyone has read what it needs of the window)
+        for (int i = tid; i < n_listed; i += kLogitsThreads) counts[i] = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) touched[tid * kOwn + i] = 0;
         __syncthreads();
     }
     }
@@ -449,19 +492,15 @@ logits_kernel(const LogitsArgs a) {
     }
 }
 
-// (a row may start up to three elements into a group)
-inline int pieces_of(int vocab, int piece) { return (int)(((long long)vocab + kGroup - 1 + piece - 1) / piece); }
-
-template <typename T, int PER>
+template <typename T>
 arb_status launch_typed(Ctx *ctx, LogitsArgs a, cudaStream_t stream) {
-    constexpr int kPc = kPiece<PER>;
-    constexpr int kSmem = kPc * (int)(sizeof(int) + sizeof(uint16_t)) + kPc / 8;   // of a call with history or biases
+    constexpr int kSmem = kCap * (int)(sizeof(int) + sizeof(uint16_t)) + kWindow * kPiece / 32 * (int)(sizeof(uint32_t) + sizeof(uint16_t));   // of a call with history or biases
     static_assert(kSmem <= 48 * 1024, "no opt-in needed");
-    a.pieces = pieces_of(a.p.vocab, kPc);
+    a.pieces = (int)(((long long)a.p.vocab + kGroup - 1 + kPiece - 1) / kPiece);   // (a row may start up to three elements into a group)
     const long long share = (long long)ctx->num_sms * kLogitsCtas / a.p.rows;
     const int runs = (int)(share < 1 ? 1 : share < a.pieces ? share : a.pieces);   // of a row
     if ((size_t)a.p.rows * runs * sizeof(Record) > ctx->chunk_ws_bytes) return ARB_ERR_WORKSPACE;
-    const cudaError_t err = launch_pdl(logits_kernel<T, PER>, dim3(runs, a.p.rows), dim3(kLogitsThreads),
+    const cudaError_t err = launch_pdl(logits_kernel<T>, dim3(runs, a.p.rows), dim3(kLogitsThreads),
                                        a.p.history || a.p.bias_offsets ? kSmem : 0, stream, a);
     ctx->launches++;
     return err == cudaSuccess ? ARB_OK : ARB_ERR_CUDA;
@@ -474,10 +513,7 @@ arb_status launch_logits(Ctx *ctx, const arb_logits_params &p, cudaStream_t stre
     a.p = p;
     a.records = reinterpret_cast<Record *>(ctx->chunk_ws);
     a.counters = ctx->counters;
-    // smaller pieces where they still find a CTA each
-    const bool few = (long long)p.rows * pieces_of(p.vocab, kPiece<2>) <= (long long)ctx->num_sms * kLogitsCtas;
-    if (p.dtype == ARB_BF16) return few ? launch_typed<__nv_bfloat16, 2>(ctx, a, stream) : launch_typed<__nv_bfloat16, 4>(ctx, a, stream);
-    return few ? launch_typed<float, 2>(ctx, a, stream) : launch_typed<float, 4>(ctx, a, stream);
+    return p.dtype == ARB_BF16 ? launch_typed<__nv_bfloat16>(ctx, a, stream) : launch_typed<float>(ctx, a, stream);
 }
 
 }  // namespace arb

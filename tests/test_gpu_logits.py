@@ -186,6 +186,20 @@ def test_a_token_listed_many_times():
     check(x, o)
 
 
+@pytest.mark.parametrize("V,n", [(4 * 4096 + 5, 12000), (9 * 4096 - 1, 5000)])
+def test_long_histories_of_many_rows(V, n):
+    """More rows than CTAs at a time, so that a CTA has many pieces, and more special tokens than it holds for all of them."""
+    r = np.random.RandomState(V)
+    S = 640
+    x = torch.from_numpy(r.randn(S, V).astype(np.float32)).bfloat16()
+    o = {"history": np.stack([r.permutation(V)[:n] for _ in range(S)]).astype(np.int32), "presence": r.rand(S).astype(np.float32)}
+    o["history_lens"] = np.where(np.arange(S) % 3 == 0, n // 8, n).astype(np.int32)
+    o["bias_offsets"] = (np.arange(S + 1) * 2).astype(np.int32)
+    o["bias_tokens"] = r.randint(0, V, 2 * S).astype(np.int32)
+    o["bias_values"] = r.randn(2 * S).astype(np.float32)
+    check(x, o)
+
+
 def test_what_is_not_wanted_is_left_out():
     x, o = inputs(8, 3, 7001, history=20)
     c, b = H.ctx(), _binding()

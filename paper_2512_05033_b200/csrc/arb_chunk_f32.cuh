@@ -15,7 +15,8 @@
 // loads of the first product are the bound there).
 //
 // Rules (template parameter RULED, arb_attn_rules): a row tile walks the hull of the keys its rows see, every row masks its own
-// range, and the cap and the bias are applied to a lane's scores before the maximum.
+// range, and the cap and the bias are applied to a lane's scores before the maximum.  Two steps of 56 and 104 tokens over 1.3k and 1.8k keys
+// (8 / 2 heads of 128) that see 640 keys back 36 us (62 over all keys; a warp per query row and head 962).
 #pragma once
 
 #include <type_traits>
@@ -489,10 +490,19 @@ arb_status launch_rows(Ctx *ctx, F32ArgsOf<RULED> a, cudaStream_t stream) {
 // and two sequences of 64 tokens over 300 keys, 200: 18.1 / 16.5 / 20.5 (24.4 / 24.5 / 32.4).  At the first line (room / 4 = 148) 16 rows
 // win by a quarter, at the second (296) 32 do against 64.  Both lie low: they were drawn where a CTA's share falls below kMinUnits,
 // and tiles of the next smaller height still win somewhat above them, the less the more row tiles the call has.
+// With rules the table's keys are at most the window's and a row tile's, and the lines lie at room / 2 and room; us with tiles of 16 / 32 /
+// 64 rows, 8 / 2 heads of 64 (of 128) and a window:
+//   one sequence, 64 tokens, window 640, 220:       15.8 / 16.4 / 20.5  (21.3 / 24.6 / 36.3)
+//   two of 56 and 104 tokens, window 640, 528:      28.1 / 24.9 / 24.2  (37.7 / 36.7 / 42.6)
+//   four of 32 to 64 tokens, window 640, 704:       34.6 / 27.5 / 24.1  (48.1 / 42.0 / 42.3)
+//   four of 32 to 96, 16 / 4 heads, window 640, 1760: 71.6 / 54.0 / 45.7  (102.9 / 85.9 / 73.4)
 template <int D, int G, bool RULED = false>
 arb_status launch_one(Ctx *ctx, const F32ArgsOf<RULED> &a, cudaStream_t stream) {
-    const long long most = (long long)a.Hkv * ((long long)a.rows * G / 64 + a.batch) * ((a.max_pages * (long long)kPage + kKeys - 1) / kKeys);
-    const long long room = (long long)kMinUnits * kCtasPerSm * ctx->num_sms;
+    long long keys = a.max_pages * (long long)kPage;
+    if constexpr (RULED)
+        if (a.rules.window > 0) keys = min(keys, (long long)a.rules.window + 64 / G);
+    const long long most = (long long)a.Hkv * ((long long)a.rows * G / 64 + a.batch) * ((keys + kKeys - 1) / kKeys);
+    const long long room = (RULED ? 2ll : 1ll) * kMinUnits * kCtasPerSm * ctx->num_sms;
     if (4 * most <= room) return launch_rows<D, G, 16, RULED>(ctx, a, stream);
     if (2 * most <= room) return launch_rows<D, G, 32, RULED>(ctx, a, stream);
     return launch_rows<D, G, 64, RULED>(ctx, a, stream);

@@ -145,7 +145,7 @@ struct RuledArgs : MmaArgs {
     float2 cap_fit[4];   // coefficients of the cap's polynomial in the square of the raw product, in both halves (see capped2)
     int cap_plain;       // they are ordinary numbers
 };
-enum { kNoRules = 0, kRules = 1, kRulesBias = 2 };   // what a kernel is compiled for: ranges and cap; and slopes
+enum { kNoRules = 0, kRange = 1, kRules = 2, kRulesBias = 3 };   // what a kernel is compiled for: ranges of keys; and a cap; and slopes
 template <bool RULED>
 using ArgsOf = std::conditional_t<RULED, RuledArgs, MmaArgs>;
 
@@ -675,7 +675,7 @@ __device__ __forceinline__ void apply_rules(const RuledArgs &a, uint32_t (&v)[kB
 template <int G, bool E4M3, int HD, int RULES>
 __global__ void __launch_bounds__(threads_of(E4M3), 1)
 chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-    constexpr bool RULED = RULES != kNoRules, BIAS = RULES == kRulesBias;
+    constexpr bool RULED = RULES != kNoRules, CAP = RULES >= kRules, BIAS = RULES == kRulesBias;
     using Sh = Shape<HD, RULED>;
     constexpr int kTileBytes = Sh::kTileBytes, kStages = Sh::kStages;
     constexpr uint32_t kPCols = Sh::kPCols, kOCol = Sh::kOCol;
@@ -1163,7 +1163,7 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
             float m_used = -INFINITY, l_sum = 0.f;
             const int ntiles = w.ntiles, t0 = w.t0, kv_len = w.kv_len, lo = RULED ? w.lo : 0;   // what the loop needs
             float scale_log2 = a.scale_log2;   // of what the rules leave in the registers
-            if constexpr (RULED) {
+            if constexpr (CAP) {
                 if (a.rules.to_cap > 0.f || (BIAS && a.rules.slopes)) scale_log2 = 1.0f;
             }
             const uint32_t it0 = it;
@@ -1186,7 +1186,7 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
                 tc_fence_before();
                 mbar_arrive(&bars->s_free[grp]);   // the next unit's S may be computed
                 bool late = false;   // RULED: the cap is taken on the way to the weights
-                if constexpr (RULED) {
+                if constexpr (CAP) {
                     const bool edge = nvis < kBN || from > key0;
                     if (a.rules.to_cap > 0.f) {
                         late = a.cap_plain && !(BIAS && a.rules.slopes) && !__any_sync(0xffffffffu, edge);
@@ -1222,7 +1222,7 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
                         mx4[u] = max3(mx4[u], __uint_as_float(v[k + 2 * u]), __uint_as_float(v[k + 2 * u + 1]));
                 }
                 float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2;  // -inf: sees nothing
-                if constexpr (RULED) {
+                if constexpr (CAP) {
                     if (late) {
                         float unused;
                         unpack_f32x2(capped2(a, both(m_tile), both(a.scale_log2), 0ull), m_tile, unused);   // (of the raw product: scale_log2 is 1)
@@ -1286,7 +1286,7 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
                     if constexpr (Sh::kSplitP) tmem_st16(p_tmem + kBN / 2 + c4 * 16, pl);
                 }
                 };
-                if constexpr (RULED) {
+                if constexpr (CAP) {
                     if (late) weights(std::true_type(), both(a.scale_log2));
                     else weights(std::false_type(), sc2);
                 } else {

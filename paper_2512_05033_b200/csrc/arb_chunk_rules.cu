@@ -18,6 +18,7 @@ arb_status launch_chunk_rules(Ctx *ctx, const arb_attn_params &p, const Rules &r
                               const void *v_pages, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens,
                               void *out, cudaStream_t stream) {
     if (rules.slopes) return launch_chunk_bias(ctx, p, rules, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
+    if (rules.to_cap <= 0.f) return launch_chunk_range(ctx, p, rules, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
     alignas(64) CUtensorMap km, vm;
     const PoolView view = p.head_dim == 64 ? PoolView::kBf16D64 : PoolView::kBf16HalfRows;
     if (!pool_map(ctx, &km, k_pages, p.num_pages, p.num_kv_heads, view) ||

@@ -45,8 +45,8 @@ __device__ __forceinline__ float tanh_any(float x) {
     return fabsf(x) <= 1.0f ? tanh_small(x) : (x == x ? big : x);
 }
 
-// Launchers (one per translation unit): decode rows of a bf16 cache, without first keys; decode rows of every type; chunks of bf16, without
-// and with slopes, of fp32
+// Launchers (one per translation unit): decode rows of a bf16 cache, without first keys; decode rows of every type; chunks of bf16 with
+// ranges alone, with a cap, with slopes; chunks of fp32
 arb_status launch_step_rules(Ctx *ctx, const arb_attn_params &p, const Rules &rules, const void *q, const void *k_pages,
                              const void *v_pages, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens,
                              void *out, cudaStream_t stream);
@@ -54,6 +54,9 @@ arb_status launch_decode_rules(Ctx *ctx, const arb_attn_params &p, const Rules &
                                const void *v_pages, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens,
                                void *out, cudaStream_t stream);
 arb_status launch_chunk_rules(Ctx *ctx, const arb_attn_params &p, const Rules &rules, const void *q, const void *k_pages,
+                              const void *v_pages, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens,
+                              void *out, cudaStream_t stream);
+arb_status launch_chunk_range(Ctx *ctx, const arb_attn_params &p, const Rules &rules, const void *q, const void *k_pages,
                               const void *v_pages, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens,
                               void *out, cudaStream_t stream);
 arb_status launch_chunk_bias(Ctx *ctx, const arb_attn_params &p, const Rules &rules, const void *q, const void *k_pages,

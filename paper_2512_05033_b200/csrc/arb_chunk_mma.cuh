@@ -599,20 +599,25 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // the weights (see `weights`): tanh is monotonic, so the maximum is taken of the raw products.  The others, which have hidden
 // keys or a bias to take in between, get it here.  Step-scoring batch (32 steps, 28 / 4 heads, cap 30): polynomial of degree 5 in a
 // pass of its own 560 us, taken on the way to the weights with the scale folded in 480, with 208 registers a softmax thread
-// (see setmaxnreg below; 168 spill) 462; without a cap 323, arb_attn's kernel 285.  The FMA pipe's 7 operations for two scores and the
-// exponentials share the time; written in strict alternation they took as long.
+// (see setmaxnreg below; 168 spill) 470, with six operations and the bound below 455; arb_attn's kernel 285.  The FMA pipe's six operations
+// for two scores and the exponentials share the time (written in strict alternation they took as long), and a tile's straight
+// way of some 900 instructions outgrows the first instruction cache.  So ranges of keys alone are a kernel without the cap's code: prompts of
+// documents 274 -> 231 us.
 // The bias.  -slope |pos - j|; keys of a tile that lies at or before the row's own key are at distance pos - key0 - k.
 constexpr float kCapPoly = 0.8f;
+// The check needs a row's largest |s|.  While that is at most this (log2 units), it stands in for the row's maximum: any bound
+// serves a softmax whose weights keep their relative precision, and these lie above 2^-48.  One pass over the scores less.
+constexpr float kBoundLog2 = 24.f;
 __device__ __forceinline__ uint64_t both(float x) { return pack_f32x2(x, x); }
-// Raw products r of two keys, |scale r| <= kCapPoly cap -> cap tanh(scale r / cap) log2 e plus add2: s + s x^2 P(x^2) with the powers of
-// scale / cap folded into the coefficients, s = scale log2 e r.  Seven operations for two keys.
+// Raw products r of two keys, |scale r| <= kCapPoly cap -> cap tanh(scale r / cap) log2 e plus add2: s (1 + x^2 P(x^2)), s = scale log2 e r,
+// with the factors of s and x folded into the coefficients.  Six operations for two keys.
 __device__ __forceinline__ uint64_t capped2(const RuledArgs &a, uint64_t r, uint64_t scale2, uint64_t add2) {
     auto c = [&](int i) { return pack_f32x2(a.cap_fit[i].x, a.cap_fit[i].y); };
     const uint64_t w = mul_f32x2(r, r);
     uint64_t p = fma_f32x2(c(3), w, c(2));
     p = fma_f32x2(p, w, c(1));
     p = fma_f32x2(p, w, c(0));
-    return fma_f32x2(mul_f32x2(r, w), p, fma_f32x2(r, scale2, add2));
+    return fma_f32x2(r, fma_f32x2(p, w, scale2), add2);
 }
 
 __device__ __forceinline__ uint64_t capped2(const MmaArgs &, uint64_t, uint64_t, uint64_t) { return 0; }   // (never called)
@@ -1185,16 +1190,21 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
                 tmem_wait_ld();
                 tc_fence_before();
                 mbar_arrive(&bars->s_free[grp]);   // the next unit's S may be computed
-                bool late = false;   // RULED: the cap is taken on the way to the weights
+                bool late = false;   // CAP: the cap is taken on the way to the weights
+                bool bounded = false;   // with a bound in place of the row's maximum
+                float big = 0.f;
                 if constexpr (CAP) {
                     const bool edge = nvis < kBN || from > key0;
                     if (a.rules.to_cap > 0.f) {
                         late = a.cap_plain && !(BIAS && a.rules.slopes) && !__any_sync(0xffffffffu, edge);
                         if (late) {
-                            float big = 0.f;
+                            float big4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int k = 0; k < kBN; k += 2) big = max3(big, fabsf(__uint_as_float(v[k])), fabsf(__uint_as_float(v[k + 1])));
+                            for (int k = 0; k < kBN; k += 2)
+                                big4[k / 2 & 3] = max3(big4[k / 2 & 3], fabsf(__uint_as_float(v[k])), fabsf(__uint_as_float(v[k + 1])));
+                            big = fmaxf(fmaxf(big4[0], big4[1]), fmaxf(big4[2], big4[3]));
                             late = !__any_sync(0xffffffffu, big * a.rules.to_cap > kCapPoly);
+                            bounded = late && !__any_sync(0xffffffffu, big * a.scale_log2 > kBoundLog2);
                         } else if (edge) {   // what hidden slots hold has no say in how a tile's scores are worked out
 #pragma unroll
                             for (int k = 0; k < kBN; ++k)
@@ -1214,14 +1224,17 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
                         if (k < from - key0) v[k] = 0xff800000u;
                 }
                 // ---- row max, four independent chains of three-input maxima
-                float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float m_tile = big;
+                if (!CAP || !bounded) {
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int k = 0; k < kBN; k += 8) {
+                    for (int k = 0; k < kBN; k += 8) {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        mx4[u] = max3(mx4[u], __uint_as_float(v[k + 2 * u]), __uint_as_float(v[k + 2 * u + 1]));
+                        for (int u = 0; u < 4; ++u)
+                            mx4[u] = max3(mx4[u], __uint_as_float(v[k + 2 * u]), __uint_as_float(v[k + 2 * u + 1]));
+                    }
+                    m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2;  // -inf: sees nothing
                 }
-                float m_tile = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * scale_log2;  // -inf: sees nothing
                 if constexpr (CAP) {
                     if (late) {
                         float unused;

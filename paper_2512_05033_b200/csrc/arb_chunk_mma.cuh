@@ -602,7 +602,7 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // (see setmaxnreg below; 168 spill) 470, with six operations and the bound below 455; arb_attn's kernel 285.  The FMA pipe's six operations
 // for two scores and the exponentials share the time (written in strict alternation they took as long), and a tile's straight
 // way of some 900 instructions outgrows the first instruction cache.  So ranges of keys alone are a kernel without the cap's code: prompts of
-// documents 274 -> 231 us.
+// documents 274 -> 231 us, the step-scoring batch with every rule off 323 -> 289.
 // The bias.  -slope |pos - j|; keys of a tile that lies at or before the row's own key are at distance pos - key0 - k.
 constexpr float kCapPoly = 0.8f;
 // The check needs a row's largest |s|.  While that is at most this (log2 units), it stands in for the row's maximum: any bound
@@ -1065,7 +1065,7 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
     } else {
         // ================================ softmax and epilogue ====================================
         if constexpr (E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-        // (2 * 208 + 88 = 3 * 168, what 384 threads start with; without it the rules' bounds spill: rules off 365 -> 325 us)
+        // (2 * 208 + 88 = 3 * 168, what 384 threads start with; without it the rules' bounds spill: rules off, with the cap's code, 365 -> 325 us)
         if constexpr (RULED) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // two groups of 128 threads: group g works on row tile g of a pair (on every second KV tile of a single row
         // tile); thread tg of a group owns TMEM lane tg

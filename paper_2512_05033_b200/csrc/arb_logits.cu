@@ -241,7 +241,8 @@ logits_kernel(const LogitsArgs a) {
     if (special) {
         const int32_t *history = p.history + (size_t)row * p.history_stride;
         const int first = max(w_lo, 0);
-        unsigned tokens_here;
+        unsigned tokens_here;   // none where a row's skew leaves its last window behind the row
+        auto here = [&](int t) { return (unsigned)t - (unsigned)first < tokens_here; };
         // f(t) for every token of a list that lies in the window, the loads of kHeld in flight together
         auto each = [&](const int32_t *tokens, int n, auto f) {
             for (int i0 = tid; i0 < n; i0 += kHeld * kLogitsThreads) {
@@ -250,13 +251,13 @@ logits_kernel(const LogitsArgs a) {
                 for (int k = 0; k < kHeld; ++k) t[k] = i0 + k * kLogitsThreads < n ? __ldg(tokens + i0 + k * kLogitsThreads) : -1;
 #pragma unroll
                 for (int k = 0; k < kHeld; ++k)
-                    if ((unsigned)(t[k] - first) < tokens_here) f(t[k] - w_lo);
+                    if (here(t[k])) f(t[k] - w_lo);
             }
         };
         auto mark = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
         auto slot_of = [&](int at) { return before[at >> 5] + __popc(touched[at >> 5] & ((1u << (at & 31)) - 1u)); };
         for (;;) {
-            tokens_here = (unsigned)(min((long long)w_end * kPc - skew, (long long)V) - first);
+            tokens_here = (unsigned)max(min(w_end * kPc - skew, V) - first, 0);
             each(history, n_history, mark);
             each(p.bias_tokens + b_begin, b_end - b_begin, mark);
             __syncthreads();
@@ -323,7 +324,7 @@ logits_kernel(const LogitsArgs a) {
         __syncthreads();
         for (int i = b_begin + tid; i < b_end; i += kLogitsThreads) {
             const int t = __ldg(p.bias_tokens + i);
-            if ((unsigned)(t - first) >= tokens_here) continue;
+            if (!here(t)) continue;
             float sum = __ldg(p.bias_values + i);
             if (again) {
                 bool earliest = true;

@@ -257,3 +257,24 @@ def test_gumbel_noise_draws_from_the_softmax():
     p = np.exp(row) / np.exp(row).sum()
     count = np.bincount(tokens.cpu().numpy(), minlength=8)
     assert count[5] == 0 and bool((np.abs(count - n * p) <= 5 * np.sqrt(n * p * (1 - p)) + 1).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("S", [1, 64, 640])
+@pytest.mark.parametrize("V", [1, 2045, 2046, 2047, 2048, 2049, 9 * 2048 - 2, 9 * 2048 - 1])
+def test_vocabularies_that_end_with_a_piece(V, S, dtype):
+    """A row may start inside a group of four tokens, so the pieces of a row that starts on one may reach past its end by a whole piece:
+    nothing of the history or the biases lies there, least of all tokens outside the vocabulary."""
+    if S == 640 and V > 4096:
+        S = 600                                          # (a run of all a row's pieces, the last in a window of its own)
+    x, o = inputs(V + S, S, V, dtype, history=40, biases=12, mask=True, temperature=True)
+    o["history"][:, 1] = np.random.RandomState(V).choice([-2 ** 31, -1, V, V + 5, V + 3000, 2 ** 31 - 1], S)
+    far = np.arange(len(o["bias_tokens"])) % 5 == 0
+    o["bias_tokens"][far] = np.random.RandomState(S).choice([-2 ** 31, -V, V, V + 1, 2 * V + 4096, 2 ** 31 - 1], far.sum())
+    check(x, o)
+
+
+@pytest.mark.parametrize("V", [126974, 126975, 151550, 151551])
+def test_large_vocabularies_that_end_with_a_piece(V):
+    check(*inputs(V, 3, V, torch.bfloat16, history=500, biases=40, temperature=True))
+    check(*inputs(V, 70, V, torch.bfloat16, history=50, biases=40))

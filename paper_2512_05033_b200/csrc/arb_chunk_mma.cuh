@@ -143,7 +143,7 @@ struct MmaArgs {
 struct RuledArgs : MmaArgs {
     Rules rules;
     float2 cap_fit[4];   // coefficients of the cap's polynomial in the square of the raw product, in both halves (see capped2)
-    int cap_plain;       // they are ordinary numbers
+    int cap_plain;       // they are ordinary numbers, and the products that they meet are
 };
 enum { kNoRules = 0, kRange = 1, kRules = 2, kRulesBias = 3 };   // what a kernel is compiled for: ranges of keys; and a cap; and slopes
 template <bool RULED>
@@ -605,6 +605,10 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // documents 274 -> 231 us, the step-scoring batch with every rule off 323 -> 289.
 // The bias.  -slope |pos - j|; keys of a tile that lies at or before the row's own key are at distance pos - key0 - k.
 constexpr float kCapPoly = 0.8f;
+// Caps up to this (1024, in log2 units) may take the form out of exponential and reciprocal, whose error of 2^-22 of the cap is then
+// a sixteenth of a weight's rounding to bf16; larger ones, and those the folded coefficients do not reach, take tanh_any, which keeps its relative
+// error down to 0.
+constexpr float kCapExpLog2 = 1024.f * 1.4426950408889634f;
 // The check needs a row's largest |s|.  While that is at most this (log2 units), it stands in for the row's maximum: any bound
 // serves a softmax whose weights keep their relative precision, and these lie above 2^-48.  One pass over the scores less.
 constexpr float kBoundLog2 = 24.f;
@@ -634,12 +638,17 @@ __device__ __forceinline__ void apply_rules(const RuledArgs &a, uint32_t (&v)[kB
                 mx4[u] = max3(mx4[u], fabsf(__uint_as_float(v[k + 2 * u])), fabsf(__uint_as_float(v[k + 2 * u + 1])));
         }
         const float big = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.rules.to_cap;
-        if (!a.cap_plain || __any_sync(0xffffffffu, big > kCapPoly)) {
-            // tanh(x) = 1 - 2 / (1 + e^(2 x)): off by 2^-23 or so absolute, which a weight in bf16 does not notice
+        const bool reach = !a.cap_plain || __any_sync(0xffffffffu, big > kCapPoly);
+        if (reach && a.rules.cap_log2 <= kCapExpLog2) {
+            // tanh(x) = 1 - 2 / (1 + e^(2 x)): off by 2^-22 or so absolute, the score by as much of the cap
             const float to_exp = a.rules.to_cap * 2.8853900817779268f;
 #pragma unroll
             for (int k = 0; k < kBN; ++k)
                 v[k] = __float_as_uint(a.rules.cap_log2 - __fdividef(2.0f * a.rules.cap_log2, 1.0f + fast_exp2(__uint_as_float(v[k]) * to_exp)));
+        } else if (reach) {
+            // of a larger cap that is too much for the rows that do not reach it: their scores are small differences of it
+#pragma unroll
+            for (int k = 0; k < kBN; ++k) v[k] = __float_as_uint(a.rules.cap_log2 * tanh_any(__uint_as_float(v[k]) * a.rules.to_cap));
         } else {
             const uint64_t scale2 = both(a.scale_log2);
 #pragma unroll
@@ -1620,8 +1629,9 @@ inline void fill_cap(RuledArgs &a) {
     a.cap_plain = to_cap > 1e-4 && to_cap < 1e2;
     for (int i = 0; i < 4; ++i) {
         power *= to_cap * to_cap;
-        const float c = a.cap_plain ? (float)(fit[i] * power) : 0.f;
-        a.cap_fit[i] = make_float2(c, c);
+        const double c = fabs(fit[i] * power);
+        if (!(c > 1.2e-38 && c < 1e38)) a.cap_plain = 0;   // (of an unusual softmax scale)
+        a.cap_fit[i] = make_float2((float)(fit[i] * power), (float)(fit[i] * power));
     }
 }
 

@@ -582,7 +582,7 @@ typedef struct {
  * rule off the result is arb_attn's, within its tolerance.  Keys before the first and behind the last key that any of a
  * sequence's tokens sees do not reach the result, whatever they hold; of the keys between the two the values have to be
  * finite (the key rows of hidden ones may hold anything).
- * Block-table entries of pages without a visible key are not read.
+ * Block-table entries of pages before the first and behind the last of these keys are not read (none at all where no token sees a key).
  * params->flags must be 0.
  * Errors: ARB_ERR_INVALID_ARG (cap outside its range, window negative), ARB_ERR_UNSUPPORTED (flags, and what arb_attn
  * does not support), ARB_ERR_WORKSPACE, ARB_ERR_CUDA.

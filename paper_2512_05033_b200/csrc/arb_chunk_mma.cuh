@@ -156,7 +156,7 @@ using ArgsOf = std::conditional_t<RULED, RuledArgs, MmaArgs>;
 struct Item {
     int b, kvh, n, L, rows_total, r_begin, rows[2], kv_len, t0, ntiles, qrow0, slot;   // ntiles < 0: there are no more
     int split;
-    int lo;   // RULED: first key any row of the pair sees (kv_len: behind the last)
+    int lo;   // RULED: first key any row of the pair sees (kv_len: behind the last; both 0 where none sees any)
 };
 
 struct Bars {
@@ -503,7 +503,7 @@ __device__ __forceinline__ int pair_kv_len(int L, int n, int rows_total, int r_b
     const int r_last = min(r_begin + 2 * kBM, rows_total) - 1;
     return L - n + r_last / G + 1;
 }
-// RULED: the hull [lo, hi) of the keys the pair's rows see, one key at least; every lane of a warp takes part
+// RULED: the hull [lo, hi) of the keys the pair's rows see; lo == hi: none of them sees any.  Every lane of a warp takes part.
 template <int G>
 __device__ __forceinline__ void pair_range(const RuledArgs &a, int b, int L, int n, int rows_total, int r_begin, int qrow0, int lane,
                                            int &lo, int &hi) {
@@ -527,7 +527,7 @@ __device__ __forceinline__ void pair_range(const RuledArgs &a, int b, int L, int
             hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, off));
         }
     }
-    if (lo >= hi) { hi = L - n + tok1 + 1; lo = hi - 1; }
+    if (lo >= hi) lo = hi = 0;
 }
 __device__ __forceinline__ int part_tiles(int L, int P) {
     const int nt = (L + kBN - 1) / kBN;
@@ -575,7 +575,7 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
         pair_range<G>(a, sb, it.L, it.n, it.rows_total, it.r_begin, it.qrow0, threadIdx.x & 31, it.lo, it.kv_len);
         const int first = it.lo / kBN, nt_pair = (it.kv_len + kBN - 1) / kBN - first, T = P > 1 ? (nt_pair + P - 1) / P : nt_pair;
         it.t0 = first + part * T;
-        it.ntiles = max(0, min(part * T + T, nt_pair) - part * T);
+        it.ntiles = max(0, min(part * T + T, nt_pair) - part * T);   // 0 of a pair that is not split: no row of it sees a key
     } else {
     it.kv_len = pair_kv_len<G>(it.L, it.n, it.rows_total, it.r_begin);   // keys the pair's last row sees
     const int nt_pair = (it.kv_len + kBN - 1) / kBN;
@@ -1139,6 +1139,11 @@ chunk_mma_kernel(const ArgsOf<RULES != kNoRules> a, const __grid_constant__ CUte
             const Item &w = E4M3 ? mine : bars->item[slot];
             if (!E4M3 && w.ntiles < 0) break;
             if (w.ntiles == 0) {   // a part the pair sees nothing of
+                if (RULED && !w.split) {   // ... or a pair that sees nothing at all: its rows are this item's to write
+                    const int rows = w.rows[grp], r_first = w.r_begin + grp * kBM;
+                    for (int row = warp_row + lane / kLanesPerRow; row < min(rows, warp_row + 32); row += kRowsPerPass)
+                        *reinterpret_cast<uint4 *>(a.out + (row_offset(w, r_first + row) + lane % kLanesPerRow * 8) * 2) = make_uint4(0, 0, 0, 0);
+                }
                 if constexpr (!E4M3) mbar_arrive(&bars->item_empty[slot]);
                 continue;
             }
@@ -1511,8 +1516,8 @@ chunk_combine_kernel(const ArgsOf<RULED> a) {
             if constexpr (RULED) {
                 int lo, hi;
                 pair_range<G>(a, sb, L, n, rows_total, r_begin, pl.row0[sb], tid & 31, lo, hi);
-                const int nt_pair = (hi + kBN - 1) / kBN - lo / kBN, Tp = (nt_pair + P - 1) / P;
-                nparts = (nt_pair + Tp - 1) / Tp;
+                const int nt_pair = (hi + kBN - 1) / kBN - lo / kBN, Tp = max((nt_pair + P - 1) / P, 1);
+                nparts = (nt_pair + Tp - 1) / Tp;   // (0: no row of the pair sees a key)
             } else {
                 const int nt_pair = (pair_kv_len<G>(L, n, rows_total, r_begin) + kBN - 1) / kBN;
                 nparts = min(P, (nt_pair + T - 1) / T);

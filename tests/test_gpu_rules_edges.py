@@ -1,5 +1,5 @@
-"""arb_attn_rules where the definition and a kernel's way to it part most easily: caps from far
-below to far above the scores.
+"""arb_attn_rules where the definition and a kernel's way to it part most easily: caps from far below to far above the scores, and
+row tiles none of whose rows sees a key.
 
 Tolerance: that of test_gpu_rules.py with another term for the cap.  The kernels work cap * tanh(s / cap) out with a relative error
 of the result of at most 2^-19 where |s| <= cap (a polynomial's 1.2e-6 and the roundings around it), or out of an exponential
@@ -115,6 +115,41 @@ def test_a_step_as_one_chunk_and_token_by_token(D, cap):
     _, bar = reference(x)
     assert H.ctx().poll_status() == 0
     assert bool(((whole.double() - single.double()).abs().cpu() <= 2 * bar).all())
+
+
+@pytest.mark.parametrize("dtype,D,new", [(BF, 128, 1), (BF, 128, 9), (BF, 128, 70), (BF, 64, 70), (F32, 64, 1), (F32, 128, 40)])
+@pytest.mark.parametrize("L", [200, 30000])
+def test_no_row_sees_a_key_and_nothing_is_looked_up(dtype, D, new, L):
+    """First keys beyond every row: rows of zeros, whatever the cache holds and whatever the table says; short contexts and ones
+    whose keys are split over several items."""
+    for rules in ({}, {"cap": 5.0}, {"slopes": True}):
+        x = Inputs(24, dtype, 8, 2, D, [L], [new], first=[L + 5] * new, **rules)
+        x.k.fill_(float("nan"))
+        x.v.fill_(float("inf"))
+        x.table.fill_(-1)
+        args, more = x.args()
+        out = torch.full_like(args[0], 5.0)
+        H.ctx().attn_rules(*args, **more, out=out)
+        assert H.ctx().poll_status() == 0
+        assert not bool(out.any()) and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 128)])
+@pytest.mark.parametrize("L", [700, 20000])
+def test_row_tiles_that_see_nothing_beside_others_that_do(dtype, D, L):
+    """Of a step of 150 tokens (600 rows of a kv head) some runs see nothing, others only the last page; keys before that page are no
+    numbers and its table entries are unset."""
+    n = 150
+    first = [L + 1] * 70 + [L - 200] * 10 + [10 ** 9] * 64 + [L - n] * 6
+    x = Inputs(25, dtype, 8, 2, D, [L, 90], [n, 30], first=first + [0] * 30, cap=9.0)
+    dead = L - 200
+    flat = torch.arange(dead)
+    page = x.table[0, flat // P].long()
+    x.k[page, :, flat % P] = float("nan")
+    x.v[page, :, flat % P] = float("nan")
+    x.table[0, :dead // P] = -7
+    out = check(x)
+    assert not bool(out[:70].any()) and not bool(out[80:144].any()) and bool(out[70:80].any()) and bool(out[144:].any())
 
 
 def test_repeated_calls_give_the_same_bits():

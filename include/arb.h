@@ -339,7 +339,8 @@ arb_status arb_route_classes(arb_ctx *ctx, int32_t dtype, int32_t mode, int32_t 
  *   new_lens   int32 [B], >= 0; total_new >= their sum (rows beyond the sum are ignored).
  * A sequence whose new tokens do not fit under its block-table row, or whose target pages lie outside
  * the pool, is left untouched (pools and length) and raises ARB_DEV_BAD_SEQ_LEN / ARB_DEV_BAD_PAGE; a
- * negative new_len raises ARB_DEV_BAD_SEQ_LEN.  Values are copied bit for bit.
+ * negative new_len raises ARB_DEV_BAD_SEQ_LEN.  So does a sequence whose rows end behind total_new (lengths on
+ * the device that add up to more than the host said): it is left untouched too.  Values are copied bit for bit.
  */
 arb_status arb_kv_append(arb_ctx *ctx, const arb_attn_params *params, int32_t total_new, const void *k_new,
                          const void *v_new, const int32_t *block_table, int32_t *seq_lens, const int32_t *new_lens,

@@ -27,7 +27,7 @@ struct AppendArgs {
 // The tables every CTA derives, in shared memory.
 struct AppendPlan {
     int *pref;    // [B + 1] new rows before sequence b; at most total_new, whatever the lengths on the device add up to
-    int *okay;    // [B] the sequence's new tokens may be written
+    int *okay;    // [B] the sequence's new tokens may be written: they fit its table row, its pages exist, its rows are there
     int *start;   // [B] tokens it holds
 };
 
@@ -37,6 +37,7 @@ __device__ __forceinline__ int capped_sum(int a, int b, int most) { return (int)
 __device__ __forceinline__ AppendPlan append_plan(const AppendArgs &a, int *tables) {
     const int tid = threadIdx.x, lane = tid & 31, B = a.batch;
     const AppendPlan pl = {tables, tables + B + 1, tables + 2 * B + 1};
+    const int behind = a.total_new + (a.total_new < INT32_MAX);   // where the sums stop: one row behind the last
     if (tid == 0) pl.pref[0] = 0;
     // as many lanes per sequence as the block has to spare, at most a warp: each looks at every g-th of its pages
     int g = 32;
@@ -61,7 +62,7 @@ __device__ __forceinline__ AppendPlan append_plan(const AppendArgs &a, int *tabl
             if (bad && blockIdx.x == 0) atomicOr(a.status, bad);
             pl.okay[b] = bad == 0;
             pl.start[b] = L;
-            pl.pref[b + 1] = n > 0 ? min(n, a.total_new) : 0;
+            pl.pref[b + 1] = n > 0 ? min(n, behind) : 0;
         }
     }
     __syncthreads();
@@ -69,14 +70,21 @@ __device__ __forceinline__ AppendPlan append_plan(const AppendArgs &a, int *tabl
         int carry = 0;
         for (int b0 = 0; b0 < B; b0 += 32) {
             const int b = b0 + lane;
-            int v = b < B ? pl.pref[b + 1] : 0;
+            const int n = b < B ? pl.pref[b + 1] : 0;
+            int v = n;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const int t = __shfl_up_sync(0xffffffffu, v, off);
-                if (lane >= off) v = capped_sum(v, t, a.total_new);
+                if (lane >= off) v = capped_sum(v, t, behind);
             }
-            v = capped_sum(v, carry, a.total_new);
-            if (b < B) pl.pref[b + 1] = v;
+            v = capped_sum(v, carry, behind);
+            if (b < B) {
+                if (n > 0 && v > a.total_new) {   // some of its rows, or all, are not there
+                    if (blockIdx.x == 0) atomicOr(a.status, (uint32_t)ARB_DEV_BAD_SEQ_LEN);
+                    pl.okay[b] = 0;
+                }
+                pl.pref[b + 1] = min(v, a.total_new);
+            }
             carry = __shfl_sync(0xffffffffu, v, 31);
         }
     }

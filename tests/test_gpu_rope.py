@@ -296,3 +296,45 @@ def test_the_attention_reads_what_was_written():
             want = torch.softmax(s, -1) @ v[rows, h // 4].double().cpu()
             # q, k and the weights rounded to bf16: 2^-8 each of scores up to |q| |k| / sqrt(D) <= 40 and of weights
             assert float((out[rows, h].double().cpu() - want).abs().max()) < 6e-2
+
+
+@pytest.mark.parametrize("kind", ["rope", "rope_e4m3", "rope_i4", "append", "append_e4m3", "append_i4"])
+def test_sequences_whose_rows_are_not_there_are_refused(kind):
+    """new_lens on the device that fit the block table but add up to more than the rows of the call: sequences that end behind the last
+    row keep their pools and lengths and raise the bad-length bit, the others are written."""
+    b, c = _binding(), H.ctx()
+    for new, total, okay in (([3, 4, 2, 3], 12, 4), ([3, 4, 5, 3], 12, 3), ([3, 4, 5, 0], 11, 2), ([13, 0, 1, 0], 12, 0), ([12, 1, 0, 0], 12, 1)):
+        d = make(10, torch.bfloat16, 4, 2, 128, [0, 17, 5, 20], [14] * 4, 128)
+        q, k, v = (t[:total].contiguous() for t in views(d))
+        table, lens, n = d["table"].cuda(), d["before"].cuda(), torch.tensor(new, dtype=torch.int32, device="cuda")
+        bf = dict(dtype=torch.bfloat16, device="cuda")
+        pools = [torch.full((d["pages"], 2, P, 128), 3.0, **bf) for _ in range(2)]
+        codes = [torch.full((d["pages"], 2, P, 64 if kind.endswith("i4") else 128), 7, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scales = [torch.full((d["pages"], 2, P), 7.0, device="cuda") for _ in range(2)]
+        freq = d["inv_freq"].cuda()
+        if kind == "rope":
+            out = c.rope_append(q, k, v, freq, table, lens, n, *pools)
+        elif kind == "rope_e4m3":
+            out = c.rope_append_e4m3(q, k, v, freq, 16.0, 16.0, table, lens, n, *codes)
+        elif kind == "rope_i4":
+            out = c.rope_append_i4(q, k, v, freq, table, lens, n, *codes, *scales)
+        elif kind == "append":
+            c.kv_append(k, v, table, lens, n, *pools)
+        elif kind == "append_e4m3":
+            c.kv_append_e4m3(k, v, 16.0, 16.0, table, lens, n, *codes)
+        else:
+            c.kv_append_i4(k, v, table, lens, n, *codes, *scales)
+        rows, ends = [], np.cumsum(new)
+        for s in range(4):
+            rows.append(int(d["before"][s]) + (new[s] if ends[s] <= total else 0))
+        short = [s for s in range(4) if new[s] and ends[s] > total]
+        assert c.poll_status() == (b.DEV_BAD_SEQ_LEN if short else 0)
+        assert lens.tolist() == rows
+        pool = pools[0] if kind in ("rope", "append") else codes[0]
+        base = 3 if kind in ("rope", "append") else 7
+        touched = set((pool != base).any(-1).any(1).reshape(-1).nonzero().flatten().tolist())
+        written = {int(d["table"][s, p // P]) * P + p % P for s in range(4) if s not in short for p in range(int(d["before"][s]), int(d["before"][s]) + new[s])}
+        assert touched == written
+        if kind.startswith("rope"):
+            full = int(ends[max((s for s in range(4) if ends[s] <= total), default=0)]) if ends[0] <= total else 0
+            assert not bool(out[full:].any()) if short else bool(out[:full].any())

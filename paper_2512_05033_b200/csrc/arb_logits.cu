@@ -6,7 +6,7 @@
 // for a window of up to kWindow pieces: the CTA marks each in a bitmap in shared memory; the number of bits before its own
 // is a special token's slot, whichever thread comes first; a second look at the lists counts occurrences (integer atomics: any
 // order gives the same), and the slots get their penalties and biases (each bias added by any thread, unless a token is
-// listed twice: then its first entry's thread sums them up in the order of the list).  The stream over the pieces, which does
+// listed more than once: the sums of such tokens are taken by the warps, each for its own slots, which go through the list in order).  The stream over the pieces, which does
 // temperature, mask, noise, maximum and sum, takes a marked token's value from its slot.  A window with more special tokens than
 // slots is done a piece at a time.  A history is read by every CTA of its row, from L2.  The runs' records (maximum, sum,
 // best) go to the workspace; the CTA of a row that arrives last at the row's counter puts them together, run by run in order.
@@ -38,6 +38,7 @@ constexpr int kAhead = 2;                                   // pieces asked into
 constexpr int kCap = 4096;                                  // special tokens of a window, a piece's at least
 constexpr int kWindow = 8;                                  // pieces whose special tokens are found together
 constexpr int kHeld = 4;                                    // history tokens of a thread in flight
+constexpr int kWalk = 4;                                    // entries of a lane in flight where a list is gone through in order
 constexpr int kBiasOne = 1 << 24;                           // in a token's counter: occurrences in the history below, listed among the biases
 
 struct Record {      // what a run leaves of a row: max and sum of exponentials of x, the best x + noise with its token and its x
@@ -171,6 +172,49 @@ __device__ __forceinline__ void best_of(Record &r, const float (&x)[kGroup], flo
     }
 }
 
+__device__ __forceinline__ bool in_window(int t, int first, unsigned tokens) { return (unsigned)t - (unsigned)first < tokens; }
+// the slot of a marked token: the number of bits before its own
+__device__ __forceinline__ int slot_at(const uint32_t *touched, const uint16_t *before, int at) {
+    return before[at >> 5] + __popc(touched[at >> 5] & ((1u << (at & 31)) - 1u));
+}
+
+struct Window {
+    const uint32_t *touched;
+    const uint16_t *before;
+    int first, lo;     // first token of the row in it; where its bits start
+    unsigned tokens;
+};
+
+// Adds the n listed values of every slot in `twice` to its sum, in the order of the list: a warp takes its own slots, 32 entries
+// at a time, and of those the entries of one slot one after the other.  Two rows, one with a list of 60000 tokens: 0.15 ms; with one of them
+// twice 0.46 ms (a thread per entry that looks for its first and for its others: 424 ms), one token 60000 times 2.4 ms.  The room that sums
+// and bits take and the code cost the batch with every option 1 us (33 -> 34).
+__device__ __forceinline__ void add_in_order(const int32_t *tokens, const float *values, int n, const Window w, const uint32_t *twice, float *sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i0 = 0; i0 < n; i0 += 32 * kWalk) {
+        int slot[kWalk];
+#pragma unroll
+        for (int k = 0; k < kWalk; ++k) slot[k] = i0 + 32 * k + lane < n ? __ldg(tokens + i0 + 32 * k + lane) : -1;
+#pragma unroll
+        for (int k = 0; k < kWalk; ++k) {
+            const int t = slot[k];
+            slot[k] = in_window(t, w.first, w.tokens) ? slot_at(w.touched, w.before, t - w.lo) : -1;
+            if (slot[k] >= 0 && (slot[k] % (kLogitsThreads / 32) != warp || !(twice[slot[k] >> 5] >> (slot[k] & 31) & 1u))) slot[k] = -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kWalk; ++k) {
+            if (!__any_sync(0xffffffffu, slot[k] >= 0)) continue;
+            const float value = slot[k] >= 0 ? __ldg(values + i0 + 32 * k + lane) : 0.f;
+            const uint32_t alike = __match_any_sync(0xffffffffu, slot[k]);
+            const int rank = slot[k] >= 0 ? __popc(alike & ((1u << lane) - 1u)) : -1, most = __reduce_max_sync(0xffffffffu, rank);
+            for (int r = 0; r <= most; ++r) {
+                if (rank == r) sums[slot[k]] = __fadd_rn(sums[slot[k]], value);
+                __syncwarp();
+            }
+        }
+    }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kLogitsThreads, kLogitsCtas)
 logits_kernel(const LogitsArgs a) {
@@ -183,6 +227,8 @@ logits_kernel(const LogitsArgs a) {
     uint16_t *before = reinterpret_cast<uint16_t *>(touched + kWords);        // [kWords] bits set in the words before
     uint16_t *list = before + kWords;                                         // [kCap] the special tokens in their order
     float *xs = reinterpret_cast<float *>(counts);
+    float *sums = reinterpret_cast<float *>(list + kCap);                     // [kCap] with biases: what a token that is listed more than once gets
+    uint32_t *twice = reinterpret_cast<uint32_t *>(sums + kCap);              // [kCap / 32] with biases: a bit per slot of such a token
     __shared__ Record warp_rec[kWarps];
     __shared__ int warp_bits[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = p.vocab, row = blockIdx.y, runs = gridDim.x;
@@ -203,6 +249,7 @@ logits_kernel(const LogitsArgs a) {
         for (int i = 0; i < kCap / 4 / kLogitsThreads; ++i) reinterpret_cast<uint4 *>(counts)[i * kLogitsThreads + tid] = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) touched[i * kLogitsThreads + tid] = 0;
+        if (p.bias_offsets && tid < kCap / 32) twice[tid] = 0;
         __syncthreads();
     }
     wait_for_predecessor();
@@ -242,7 +289,7 @@ logits_kernel(const LogitsArgs a) {
         const int32_t *history = p.history + (size_t)row * p.history_stride;
         const int first = max(w_lo, 0);
         unsigned tokens_here;   // none where a row's skew leaves its last window behind the row
-        auto here = [&](int t) { return (unsigned)t - (unsigned)first < tokens_here; };
+        auto here = [&](int t) { return in_window(t, first, tokens_here); };
         // f(t) for every token of a list that lies in the window, the loads of kHeld in flight together
         auto each = [&](const int32_t *tokens, int n, auto f) {
             for (int i0 = tid; i0 < n; i0 += kHeld * kLogitsThreads) {
@@ -255,7 +302,7 @@ logits_kernel(const LogitsArgs a) {
             }
         };
         auto mark = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
-        auto slot_of = [&](int at) { return before[at >> 5] + __popc(touched[at >> 5] & ((1u << (at & 31)) - 1u)); };
+        auto slot_of = [&](int at) { return slot_at(touched, before, at); };
         for (;;) {
             tokens_here = (unsigned)max(min(w_end * kPc - skew, V) - first, 0);
             each(history, n_history, mark);
@@ -304,10 +351,13 @@ logits_kernel(const LogitsArgs a) {
             atomicAdd(&counts[slot], 1);
             list[slot] = (uint16_t)at;   // (whoever else writes it writes the same)
         });
-        bool again = false;   // a token is listed twice among the biases
+        bool again = false;   // a token is listed more than once among the biases
         each(p.bias_tokens + b_begin, b_end - b_begin, [&](int at) {
             const int slot = slot_of(at);
-            again = atomicOr(&counts[slot], kBiasOne) >= kBiasOne || again;
+            if (atomicOr(&counts[slot], kBiasOne) >= kBiasOne) {
+                atomicOr(&twice[slot >> 5], 1u << (slot & 31));
+                again = true;
+            }
             list[slot] = (uint16_t)at;
         });
         again = __syncthreads_or(again);
@@ -320,21 +370,21 @@ logits_kernel(const LogitsArgs a) {
                 v = __fsub_rn(v, __fmul_rn(frequency, (float)c));
             }
             xs[i] = v;
+            if (again) sums[i] = -0.0f;   // (what adds nothing to any value, a zero's sign included)
         }
         __syncthreads();
+        auto repeated = [&](int slot) { return again && (twice[slot >> 5] >> (slot & 31) & 1u); };
         for (int i = b_begin + tid; i < b_end; i += kLogitsThreads) {
             const int t = __ldg(p.bias_tokens + i);
             if (!here(t)) continue;
-            float sum = __ldg(p.bias_values + i);
-            if (again) {
-                bool earliest = true;
-                for (int j = b_begin; j < i && earliest; ++j) earliest = __ldg(p.bias_tokens + j) != t;
-                if (!earliest) continue;
-                for (int j = i + 1; j < b_end; ++j)
-                    if (__ldg(p.bias_tokens + j) == t) sum = __fadd_rn(sum, __ldg(p.bias_values + j));
-            }
             const int slot = slot_of(t - w_lo);
-            xs[slot] = __fadd_rn(xs[slot], sum);
+            if (!repeated(slot)) xs[slot] = __fadd_rn(xs[slot], __ldg(p.bias_values + i));
+        }
+        if (again) {   // (the same for the whole block)
+            add_in_order(p.bias_tokens + b_begin, p.bias_values + b_begin, b_end - b_begin, Window{touched, before, first, w_lo, tokens_here}, twice, sums);
+            __syncthreads();
+            for (int i = tid; i < n_listed; i += kLogitsThreads)
+                if (repeated(i)) xs[i] = __fadd_rn(xs[i], sums[i]);
         }
         if (p.bias_offsets) __syncthreads();
     }
@@ -460,6 +510,7 @@ logits_kernel(const LogitsArgs a) {
         for (int i = tid; i < n_listed; i += kLogitsThreads) counts[i] = 0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) touched[tid * kOwn + i] = 0;
+        if (p.bias_offsets && tid < kCap / 32) twice[tid] = 0;
         __syncthreads();
     }
     }
@@ -496,13 +547,15 @@ logits_kernel(const LogitsArgs a) {
 template <typename T>
 arb_status launch_typed(Ctx *ctx, LogitsArgs a, cudaStream_t stream) {
     constexpr int kSmem = kCap * (int)(sizeof(int) + sizeof(uint16_t)) + kWindow * kPiece / 32 * (int)(sizeof(uint32_t) + sizeof(uint16_t));   // of a call with history or biases
-    static_assert(kSmem <= 48 * 1024, "no opt-in needed");
+    constexpr int kSmemBiases = kCap * (int)sizeof(float) + kCap / 8;                                                                       // ... and what biases need besides
+    static_assert(kSmem + kSmemBiases <= 48 * 1024 && kSmem % 4 == 0, "no opt-in needed");
+    static_assert(kCap / 32 <= kLogitsThreads, "a word of a thread");
+    const int smem = a.p.bias_offsets ? kSmem + kSmemBiases : a.p.history ? kSmem : 0;
     a.pieces = (int)(((long long)a.p.vocab + kGroup - 1 + kPiece - 1) / kPiece);   // (a row may start up to three elements into a group)
     const long long share = (long long)ctx->num_sms * kLogitsCtas / a.p.rows;
     const int runs = (int)(share < 1 ? 1 : share < a.pieces ? share : a.pieces);   // of a row
     if ((size_t)a.p.rows * runs * sizeof(Record) > ctx->chunk_ws_bytes) return ARB_ERR_WORKSPACE;
-    const cudaError_t err = launch_pdl(logits_kernel<T>, dim3(runs, a.p.rows), dim3(kLogitsThreads),
-                                       a.p.history || a.p.bias_offsets ? kSmem : 0, stream, a);
+    const cudaError_t err = launch_pdl(logits_kernel<T>, dim3(runs, a.p.rows), dim3(kLogitsThreads), smem, stream, a);
     ctx->launches++;
     return err == cudaSuccess ? ARB_OK : ARB_ERR_CUDA;
 }

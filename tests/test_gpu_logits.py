@@ -278,3 +278,36 @@ def test_vocabularies_that_end_with_a_piece(V, S, dtype):
 def test_large_vocabularies_that_end_with_a_piece(V):
     check(*inputs(V, 3, V, torch.bfloat16, history=500, biases=40, temperature=True))
     check(*inputs(V, 70, V, torch.bfloat16, history=50, biases=40))
+
+
+def _events_ms(f):
+    f()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    f()
+    b.record()
+    b.synchronize()
+    return a.elapsed_time(b)
+
+
+@pytest.mark.parametrize("repeats", ["one", "pairs", "many", "all"])
+def test_long_lists_of_biases_with_repeats(repeats):
+    """A list as long as the vocabulary: with one token in it twice, with every token twice, with one token 20000 times, of one
+    token alone.  Sums are taken in the order of the list; a call takes about as long as one without repeats, not the square of it."""
+    V, r = 60001, np.random.RandomState(3)
+    if repeats == "one":
+        tokens = np.concatenate((r.permutation(V), [V // 2]))
+    elif repeats == "pairs":
+        tokens = np.concatenate((r.permutation(V), r.permutation(V)))
+    elif repeats == "many":
+        tokens = r.permutation(np.concatenate((np.arange(V), np.full(20000, 1234))))
+    else:
+        tokens = np.full(V, 777)
+    n = len(tokens)
+    o = {"bias_offsets": np.array([0, 3, n + 3], np.int32), "bias_tokens": np.concatenate(([5, 6, 5], tokens)).astype(np.int32),
+         "bias_values": r.randn(n + 3).astype(np.float32)}
+    x = torch.from_numpy(r.randn(2, V).astype(np.float32))
+    check(x, o)
+    d = {k: torch.from_numpy(v).cuda() for k, v in o.items()}
+    xs = x.cuda()
+    assert _events_ms(lambda: H.ctx().logits(xs, **d)) < 25.0

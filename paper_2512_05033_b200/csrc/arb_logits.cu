@@ -554,7 +554,8 @@ arb_status launch_typed(Ctx *ctx, LogitsArgs a, cudaStream_t stream) {
     a.pieces = (int)(((long long)a.p.vocab + kGroup - 1 + kPiece - 1) / kPiece);   // (a row may start up to three elements into a group)
     const long long share = (long long)ctx->num_sms * kLogitsCtas / a.p.rows;
     const int runs = (int)(share < 1 ? 1 : share < a.pieces ? share : a.pieces);   // of a row
-    if ((size_t)a.p.rows * runs * sizeof(Record) > ctx->chunk_ws_bytes) return ARB_ERR_WORKSPACE;
+    const bool records = runs > 1 && (a.p.tokens || a.p.logprobs);   // a row of one run, or whose token nobody wants, leaves none
+    if (records && (size_t)a.p.rows * runs * sizeof(Record) > ctx->chunk_ws_bytes) return ARB_ERR_WORKSPACE;
     const cudaError_t err = launch_pdl(logits_kernel<T>, dim3(runs, a.p.rows), dim3(kLogitsThreads), smem, stream, a);
     ctx->launches++;
     return err == cudaSuccess ? ARB_OK : ARB_ERR_CUDA;

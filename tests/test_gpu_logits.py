@@ -311,3 +311,15 @@ def test_long_lists_of_biases_with_repeats(repeats):
     d = {k: torch.from_numpy(v).cuda() for k, v in o.items()}
     xs = x.cuda()
     assert _events_ms(lambda: H.ctx().logits(xs, **d)) < 25.0
+
+
+def test_rows_that_leave_no_records_ask_for_no_workspace():
+    """A context with a small workspace serves calls whose rows are each one CTA's, and calls that want the logits alone."""
+    c = _binding().Context(0, workspace_bytes=64 << 10)
+    x, o = inputs(11, 9000, 70, history=5)
+    want, wt, _ = reference(x.numpy(), **o)
+    d = {k: torch.from_numpy(v).cuda() for k, v in o.items()}
+    out, tokens, _ = c.logits(x.cuda(), **d)
+    assert np.array_equal(out.cpu().numpy(), want) and np.array_equal(tokens.cpu().numpy(), wt)
+    assert c.poll_status() == 0
+    c.close()

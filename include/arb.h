@@ -638,8 +638,8 @@ typedef struct {
  * last puts the others' maxima and sums together, always in the same order.  Uses the ctx's arrival counters and step
  * workspace.  Calls with other options or sizes cut rows elsewhere: logprobs then agree within rounding, the rest bit for bit.
  * Errors: ARB_ERR_INVALID_ARG (no logits, nothing wanted, bad sizes or strides, bias or history incomplete),
- * ARB_ERR_UNSUPPORTED (dtype, more than 65535 rows, vocab or
- * history_stride of 2^24 and more), ARB_ERR_WORKSPACE, ARB_ERR_CUDA.
+ * ARB_ERR_UNSUPPORTED (dtype, more than 65535 rows, a vocab of more than 2^24, a history_stride of 2^24 and more, a bias_total of 2^30 and more),
+ * ARB_ERR_WORKSPACE, ARB_ERR_CUDA.
  */
 arb_status arb_logits(arb_ctx *ctx, const arb_logits_params *params, arb_stream_t stream);
 

@@ -839,7 +839,7 @@ arb_status arb_logits(arb_ctx *ctx, const arb_logits_params *params, arb_stream_
     const arb_logits_params &p = *params;
     if (p.dtype != ARB_F32 && p.dtype != ARB_BF16) return ARB_ERR_UNSUPPORTED;
     if (p.rows < 0 || p.vocab < 1 || (p.logits_stride != 0 && p.logits_stride < p.vocab)) return ARB_ERR_INVALID_ARG;
-    if (p.rows > 65535 || p.vocab > (1 << 24) || p.history_stride >= (1 << 24)) return ARB_ERR_UNSUPPORTED;
+    if (p.rows > 65535 || p.vocab > (1 << 24) || p.history_stride >= (1 << 24) || p.bias_total >= (1 << 30)) return ARB_ERR_UNSUPPORTED;
     if (p.history ? p.history_stride < 1 : p.history_lens != nullptr) return ARB_ERR_INVALID_ARG;
     if (p.bias_offsets ? (p.bias_total < 0 || (p.bias_total > 0 && (!p.bias_tokens || !p.bias_values)))
                        : (p.bias_tokens || p.bias_values))

@@ -449,6 +449,17 @@ METHOD(spearman) {
     });
 }
 
+// lengths that the records hold in 32 bits
+int length(int64_t n, const char *name) {
+    if (n > INT32_MAX) fail(PyExc_ValueError, "%s is too long", name);
+    return (int)n;
+}
+bool truth(PyObject *o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised();
+    return v != 0;
+}
+
 // Tensors of the calls below live on the context's device, which the Python side passes as a number.
 void *on(const at::Tensor &t, const char *name, int device) {
     void *p = dev(t, name);
@@ -531,7 +542,7 @@ METHOD(rope_append) {
         r.q_weight = F32(sized_or_null(a[16], "q_weight", device, at::kFloat, D));
         r.k_weight = F32(sized_or_null(a[17], "k_weight", device, at::kFloat, D));
         r.eps = to_float(a[18]);
-        r.interleaved = PyObject_IsTrue(a[19]);
+        r.interleaved = truth(a[19]);
         r.positions = I32(sized_or_null(a[20], "positions", device, kI32, T));
         r.q_stride = qr.stride; r.k_stride = kr.stride; r.v_stride = vr.stride;
         const float ki = to_float(a[7]), vi = to_float(a[8]);
@@ -543,7 +554,7 @@ METHOD(rope_append) {
             vs = sized(a[15], "v_scales", device, at::kFloat, kp.size(0) * hkv * kp.size(2));
         }
         void *qo = sized(a[21], "q_out", device, dt, T * hq * D);
-        const int update = PyObject_IsTrue(a[22]);
+        const int update = truth(a[22]);
         arb_ctx *h = context(a[0]);
         arb_stream_t s = stream_on(a[23], device);
         return without_gil([&] {
@@ -598,7 +609,7 @@ METHOD(logits) {
             const at::Tensor &hist = of_rank(tensor(a[3], "history"), 2, "history");
             if (hist.size(1) > 0) {
                 p.history = I32(sized(hist, "history", device, kI32, S * hist.size(1)));
-                p.history_stride = (int)hist.size(1);
+                p.history_stride = length(hist.size(1), "history");
                 p.history_lens = I32(sized_or_null(a[4], "history_lens", device, kI32, S));
             }
         } else if (a[4] != Py_None) {
@@ -611,16 +622,16 @@ METHOD(logits) {
             fail(PyExc_ValueError, "%s", "bias_offsets, bias_tokens and bias_values go together");
         if (a[8] != Py_None) {
             const at::Tensor &tokens = tensor(a[9], "bias_tokens");
+            p.bias_total = length(tokens.numel(), "bias_tokens");
             p.bias_offsets = I32(sized(a[8], "bias_offsets", device, kI32, S + 1));
             p.bias_tokens = I32(on(tokens, "bias_tokens", device, kI32));
             p.bias_values = F32(sized(a[10], "bias_values", device, at::kFloat, tokens.numel()));
-            p.bias_total = (int)tokens.numel();
         }
         if (a[11] != Py_None) {
             const at::Tensor &mask = of_rank(tensor(a[11], "mask"), 2, "mask");
             if (mask.size(1) * 32 < V) fail(PyExc_ValueError, "%s", "mask has too few words for the vocabulary");
             p.mask = static_cast<uint32_t *>(sized(mask, "mask", device, kI32, S * mask.size(1)));
-            p.mask_stride = (int)mask.size(1);
+            p.mask_stride = length(mask.size(1), "mask");
         }
         p.temperature = F32(sized_or_null(a[12], "temperature", device, at::kFloat, S));
         p.noise = F32(sized_or_null(a[13], "noise", device, at::kFloat, S * V));

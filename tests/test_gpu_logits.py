@@ -323,3 +323,24 @@ def test_rows_that_leave_no_records_ask_for_no_workspace():
     assert np.array_equal(out.cpu().numpy(), want) and np.array_equal(tokens.cpu().numpy(), wt)
     assert c.poll_status() == 0
     c.close()
+
+
+def test_lengths_beyond_32_bits_are_refused_and_flags_raise_their_own_error():
+    c, x = H.ctx(), torch.zeros(1, 70, device="cuda")
+    long = lambda *shape: torch.zeros(1, dtype=torch.int32, device="cuda").expand(*shape)  # noqa: E731
+    off = torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="too long"):
+        c.logits(x, bias_offsets=off, bias_tokens=long(2 ** 32 + 1), bias_values=torch.zeros(1, device="cuda"))
+    for more in ({"history": long(1, 2 ** 32 + 5)}, {"mask": long(1, 2 ** 32 + 5)}):
+        with pytest.raises(ValueError):
+            c.logits(x, **more)
+
+    class Neither:
+        def __bool__(self):
+            raise ValueError("neither true nor false")
+
+    q, kv = torch.zeros(1, 4, 128, device="cuda"), torch.zeros(1, 2, 128, device="cuda")
+    pool, table, lens = torch.zeros(1, 2, 16, 128, device="cuda"), torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for flag in ("interleaved", "update_lens"):
+        with pytest.raises(ValueError, match="neither"):
+            c.rope_append(q, kv, kv, torch.zeros(64, device="cuda"), table, lens, lens, pool, pool.clone(), **{flag: Neither()})

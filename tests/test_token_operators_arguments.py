@@ -189,3 +189,10 @@ def test_logits_refusals():
 def test_the_records_match_the_header():
     b = _binding()
     assert ctypes.sizeof(b.RopeParams) == 72 and ctypes.sizeof(b.ScoreRules) == 32 and ctypes.sizeof(b.LogitsParams) == 152
+
+
+def test_lists_beyond_32_bits_are_refused():
+    """In the C ABI, whose kernels step through a list with 32-bit numbers, and in the binding, where a longer tensor's length would wrap."""
+    long_list = {"bias_offsets": PTR, "bias_tokens": PTR, "bias_values": PTR}
+    assert _logits(**long_list, bias_total=1 << 30) == UNSUPPORTED and _logits(**long_list, bias_total=2 ** 31 - 1) == UNSUPPORTED
+    assert _logits(history=PTR, history_stride=1 << 24) == UNSUPPORTED

@@ -18,6 +18,11 @@ arb_status launch_attn_rules(Ctx *ctx, const arb_attn_params &p, const arb_score
         if (st != ARB_OK) return st;
     }
     if (p.max_q_len < 2) return ARB_OK;
+    // With every rule off a chunk is arb_attn's, bit for bit (the rules' kernel has one bf16 term of the weights at 64 dimensions, where that
+    // kernel has two).
+    const bool off = !(rules.cap > 0.f) && rules.window == 0 && !rules.slopes && !rules.prefix_lens && !rules.first_keys;
+    if (off && p.dtype == ARB_F32) return launch_chunk_f32(ctx, p, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
+    if (off && chunk_mma_supported(p)) return launch_chunk_mma(ctx, p, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, false, stream);
     if (p.dtype == ARB_F32) return launch_chunk_f32_rules(ctx, p, r, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);
     if (!chunk_mma_supported(p)) return ARB_ERR_UNSUPPORTED;
     return launch_chunk_rules(ctx, p, r, q, k_pages, v_pages, block_table, seq_lens, q_lens, out, stream);

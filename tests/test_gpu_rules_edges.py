@@ -172,3 +172,19 @@ def test_repeated_calls_give_the_same_bits():
             else:
                 assert torch.equal(out, want[i]), (turn, i)
     assert H.ctx().poll_status() == 0
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,D", [(BF, 32, 8, 64), (BF, 28, 4, 128), (F32, 8, 2, 64)])
+def test_chunks_with_every_rule_off_are_the_plain_attentions(dtype, hq, hkv, D):
+    """Bit for bit; 64-dimension heads so at that call's bar of 1e-3 beside the output's rounding (their weights are two bf16 terms, 16
+    bits), 128-dimension ones within this module's: a weight of one bf16 term is off by up to 2^-8, which of a few keys with values of up to 4.5
+    is more than any bar of 1e-3 allows (2^-8 * 4.5 = 0.018)."""
+    x = Inputs(31, dtype, hq, hkv, D, [12, 300, 700, 2000, 40], [12, 30, 129, 16, 40])
+    args, rules = x.args()
+    a, b = H.ctx().attn(*args), H.ctx().attn_rules(*args)
+    assert H.ctx().poll_status() == 0 and torch.equal(a, b)
+    ref, bar = reference(x)
+    err = (b.double().cpu() - ref).abs()
+    assert bool((err <= bar).all())
+    if D == 64:
+        assert bool((err <= torch.finfo(dtype).eps / 2 * ref.abs() + (1e-5 if dtype == F32 else 1e-3)).all())

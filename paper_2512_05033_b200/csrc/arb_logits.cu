@@ -51,6 +51,7 @@ struct LogitsArgs {
     arb_logits_params p;
     Record *records;     // [rows][runs]
     int *counters;
+    uint32_t *status;    // of the bounds-check build
     int pieces;          // of a row
 };
 
@@ -301,8 +302,13 @@ logits_kernel(const LogitsArgs a) {
                     if (here(t[k])) f(t[k] - w_lo);
             }
         };
-        auto mark = [&](int at) { atomicOr(&touched[at >> 5], 1u << (at & 31)); };
-        auto slot_of = [&](int at) { return slot_at(touched, before, at); };
+        auto mark = [&](int at) {
+            if (ARB_IN_RANGE(a.status, at >> 5, kWords)) atomicOr(&touched[at >> 5], 1u << (at & 31));
+        };
+        auto slot_of = [&](int at) {
+            const int slot = slot_at(touched, before, ARB_IN_RANGE(a.status, at >> 5, kWords) ? at : 0);
+            return ARB_IN_RANGE(a.status, slot, n_listed) ? slot : 0;
+        };
         for (;;) {
             tokens_here = (unsigned)max(min(w_end * kPc - skew, V) - first, 0);
             each(history, n_history, mark);
@@ -363,7 +369,8 @@ logits_kernel(const LogitsArgs a) {
         again = __syncthreads_or(again);
         for (int i = tid; i < n_listed; i += kLogitsThreads) {
             const int c = counts[i] & (kBiasOne - 1);
-            float v = Elt<T>::to_float(x_in[w_lo + list[i]]);
+            const int t = w_lo + list[i];
+            float v = Elt<T>::to_float(x_in[ARB_IN_RANGE(a.status, t, V) ? t : 0]);
             if (c > 0) {
                 v = v > 0.f ? __fdiv_rn(v, repetition) : __fmul_rn(v, repetition);
                 v = __fsub_rn(v, presence);
@@ -568,6 +575,7 @@ arb_status launch_logits(Ctx *ctx, const arb_logits_params &p, cudaStream_t stre
     a.p = p;
     a.records = reinterpret_cast<Record *>(ctx->chunk_ws);
     a.counters = ctx->counters;
+    a.status = ctx->status;
     return p.dtype == ARB_BF16 ? launch_typed<__nv_bfloat16>(ctx, a, stream) : launch_typed<float>(ctx, a, stream);
 }
 

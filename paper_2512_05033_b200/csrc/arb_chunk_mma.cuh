@@ -106,7 +106,9 @@ __host__ __device__ constexpr size_t slot_floats(int head_dim) { return (size_t)
 // unit take half the tensor time, so the second term is hidden under the exponentials, and the weights keep what the
 // CUDA-core kernel that served these chunks before kept (fp32, far below the rounding of the output).  Measured: the
 // step-scoring batch with 64-dimension heads 14.1 ms -> 0.42 ms, a batch of 16 short steps over 1k-8k keys 1.33 ms -> 0.09 ms.
-// RULED: P is one bf16 term at either head dimension (prompts of documents, 32 / 8 heads of 64: 409 -> 278 us).
+// RULED: P is one bf16 term at either head dimension, each weight off by up to 2^-8 of itself, as at 128 dimensions without rules.
+// Prompts of documents, 32 / 8 heads of 64: 231 us, with two terms 317 (causal prompts with slopes 432 and 559, steps in a window
+// 66 and 90); the outputs' error against 64 bits 2.0e-3 of their norm, with two terms 1.6e-3, which is their own rounding.
 template <int HD, bool RULED = false>
 struct Shape {
     static constexpr int kHalves = HD / 64;                       // 128-byte-swizzled 64-dimension pieces of a row
@@ -599,10 +601,10 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // the weights (see `weights`): tanh is monotonic, so the maximum is taken of the raw products.  The others, which have hidden
 // keys or a bias to take in between, get it here.  Step-scoring batch (32 steps, 28 / 4 heads, cap 30): polynomial of degree 5 in a
 // pass of its own 560 us, taken on the way to the weights with the scale folded in 480, with 208 registers a softmax thread
-// (see setmaxnreg below; 168 spill) 470, with six operations and the bound below 455; arb_attn's kernel 285.  The FMA pipe's six operations
-// for two scores and the exponentials share the time (written in strict alternation they took as long), and a tile's straight
-// way of some 900 instructions outgrows the first instruction cache.  So ranges of keys alone are a kernel without the cap's code: prompts of
-// documents 274 -> 231 us, the step-scoring batch with every rule off 323 -> 289.
+// (see setmaxnreg below; 168 spill) 470, with six operations and the bound below 455; arb_attn's kernel 285.  No pipe
+// is the bound of that (the busiest is at 41 %); a tile's straight way of some 900 instructions outgrows the first instruction cache, and
+// waiting for instructions is the first stall.  Strict alternation of the polynomial and the exponentials took as long.  So ranges of keys
+// alone are a kernel without the cap's code: prompts of documents 274 -> 231 us.
 // The bias.  -slope |pos - j|; keys of a tile that lies at or before the row's own key are at distance pos - key0 - k.
 constexpr float kCapPoly = 0.8f;
 // Caps up to this (1024, in log2 units) may take the form out of exponential and reciprocal, whose error of 2^-22 of the cap is then
@@ -1646,6 +1648,40 @@ inline int most_items(const MmaArgs &a, const arb_attn_params &p) {
     long long bound = (long long)p.num_kv_heads * ((long long)p.total_q * g / kBM + p.batch);
     if (a.split_cap > 0) bound *= kSplitMaxParts;   // every item of a split sequence comes once per part
     return (int)(bound < 1 ? 1 : (bound > (1 << 30) ? (1 << 30) : bound));
+}
+
+template <int G, int RULES>
+arb_status launch_ruled_g(Ctx *ctx, const RuledArgs &a, int head_dim, const CUtensorMap &km, const CUtensorMap &vm, int max_items,
+                          cudaStream_t stream) {
+    return head_dim == 64 ? launch_one<G, false, 64, RULES>(ctx, a, km, vm, max_items, stream)
+                          : launch_one<G, false, 128, RULES>(ctx, a, km, vm, max_items, stream);
+}
+
+// The rules' kernel in one of its forms; a translation unit each, which compile side by side.
+template <int RULES>
+arb_status launch_ruled(Ctx *ctx, const arb_attn_params &p, const Rules &rules, const void *q, const void *k_pages, const void *v_pages,
+                        const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens, void *out, cudaStream_t stream) {
+    alignas(64) CUtensorMap km, vm;
+    const PoolView view = p.head_dim == 64 ? PoolView::kBf16D64 : PoolView::kBf16HalfRows;
+    if (!pool_map(ctx, &km, k_pages, p.num_pages, p.num_kv_heads, view) ||
+        !pool_map(ctx, &vm, v_pages, p.num_pages, p.num_kv_heads, view))
+        return ARB_ERR_CUDA;
+    RuledArgs a;
+    fill_args(a, ctx, p, q, k_pages, v_pages, 1.0f, 1.0f, block_table, seq_lens, q_lens, out, false);
+    a.rules = rules;
+    fill_cap(a);
+    const int max_items = most_items(a, p);
+    switch (p.num_q_heads / p.num_kv_heads) {
+        case 1: return launch_ruled_g<1, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 2: return launch_ruled_g<2, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 3: return launch_ruled_g<3, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 4: return launch_ruled_g<4, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 5: return launch_ruled_g<5, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 6: return launch_ruled_g<6, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 7: return launch_ruled_g<7, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        case 8: return launch_ruled_g<8, RULES>(ctx, a, p.head_dim, km, vm, max_items, stream);
+        default: return ARB_ERR_UNSUPPORTED;
+    }
 }
 
 }  // namespace

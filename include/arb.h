@@ -508,7 +508,8 @@ arb_status arb_kv_append_i4(arb_ctx *ctx, const arb_attn_params *params, int32_t
  *   rotation  angle_p = pos * inv_freq[p], p < rot_dim / 2; the pair (a, b) number p becomes
  *             (a cos - b sin, a sin + b cos).  interleaved == 0: pair p is (p, p + rot_dim / 2); else (2p, 2p + 1).
  *             Dimensions from rot_dim on pass through.  The angle is reduced in 64 bits, so far positions lose nothing.
- * rounded once, to the type of the output.  Values are written as they are.
+ * rounded once, to the type of the output.  Values are written as they are.  Sine and cosine are off by up to 2^-20 absolute for bf16 rows (two
+ * units of 2^-24 or so for fp32), a normed value by a few units of 2^-24.
  */
 typedef struct {
     int32_t rot_dim;          /* 0 (no rotation) .. head_dim, a multiple of 16 */
@@ -580,10 +581,14 @@ typedef struct {
 
 /*
  * Arguments, layouts, status bits and asynchrony as for arb_attn (q_lens 0, 1 or a step length; bf16 or fp32); with every
- * rule off the result is arb_attn's, within its tolerance.  Keys before the first and behind the last key that any of a
+ * rule off the result is arb_attn's, within its tolerance (chunks: bit for bit).  Keys before the first and behind the last key that any of a
  * sequence's tokens sees do not reach the result, whatever they hold; of the keys between the two the values have to be
  * finite (the key rows of hidden ones may hold anything).
  * Block-table entries of pages before the first and behind the last of these keys are not read (none at all where no token sees a key).
+ * Scores, maxima, sums and outputs are fp32 until the one rounding of out.  A bf16 call's weights enter the second product rounded to
+ * bf16 (2^-8 of each at most; tokens of 64-dimension heads keep two bf16 terms, 16 bits, as arb_attn does there; tokens with
+ * first_keys keep fp32).  cap * tanh(s / cap) is off by at most 2^-19 of itself, or by 2^-21 of the cap among scores that reach 0.8
+ * of a cap of at most 1024 in a chunk.
  * params->flags must be 0.
  * Errors: ARB_ERR_INVALID_ARG (cap outside its range, window negative), ARB_ERR_UNSUPPORTED (flags, and what arb_attn
  * does not support), ARB_ERR_WORKSPACE, ARB_ERR_CUDA.
@@ -637,6 +642,9 @@ typedef struct {
  * One pass over the logits: a row's slices are adjusted, written and reduced by one or more CTAs; the one of a row that finishes
  * last puts the others' maxima and sums together, always in the same order.  Uses the ctx's arrival counters and step
  * workspace.  Calls with other options or sizes cut rows elsewhere: logprobs then agree within rounding, the rest bit for bit.
+ * A logprob is off by at most 2^-18 + 2^-22 max |x|: exponentials and the logarithm are the fast ones, off by 2^-21, so that of a token
+ * whose probability is within 2^-20 of 1 little is left but its size.  A token listed more than once among a row's biases costs a walk of
+ * the list (linear in its length).
  * Errors: ARB_ERR_INVALID_ARG (no logits, nothing wanted, bad sizes or strides, bias or history incomplete),
  * ARB_ERR_UNSUPPORTED (dtype, more than 65535 rows, a vocab of more than 2^24, a history_stride of 2^24 and more, a bias_total of 2^30 and more),
  * ARB_ERR_WORKSPACE, ARB_ERR_CUDA.

@@ -490,12 +490,17 @@ arb_status launch_rows(Ctx *ctx, F32ArgsOf<RULED> a, cudaStream_t stream) {
 // and two sequences of 64 tokens over 300 keys, 200: 18.1 / 16.5 / 20.5 (24.4 / 24.5 / 32.4).  At the first line (room / 4 = 148) 16 rows
 // win by a quarter, at the second (296) 32 do against 64.  Both lie low: they were drawn where a CTA's share falls below kMinUnits,
 // and tiles of the next smaller height still win somewhat above them, the less the more row tiles the call has.
-// With rules the table's keys are at most the window's and a row tile's, and the lines lie at room / 2 and room; us with tiles of 16 / 32 /
-// 64 rows, 8 / 2 heads of 64 (of 128) and a window:
+// With rules the table's keys are at most the window's and a row tile's, and the lines lie at room / 2 and room, with a window or without: the
+// rules' arithmetic makes a key tile dearer, so that fewer of them fill a CTA.  us with tiles of 16 / 32 / 64 rows, 8 / 2 heads of 64 (of 128);
+// 16 rows serve up to 296, 32 up to 592:
 //   one sequence, 64 tokens, window 640, 220:       15.8 / 16.4 / 20.5  (21.3 / 24.6 / 36.3)
 //   two of 56 and 104 tokens, window 640, 528:      28.1 / 24.9 / 24.2  (37.7 / 36.7 / 42.6)
 //   four of 32 to 64 tokens, window 640, 704:       34.6 / 27.5 / 24.1  (48.1 / 42.0 / 42.3)
 //   four of 32 to 96, 16 / 4 heads, window 640, 1760: 71.6 / 54.0 / 45.7  (102.9 / 85.9 / 73.4)
+//   one, 64 tokens over 300 keys, cap, 120:         12.8 / 15.2 / 19.7  (16.6 / 23.4 / 32.0)
+//   one, 64 over 900, cap, 310:                     19.1 / 16.9 / 22.9  (26.7 / 26.0 / 44.7)
+//   two, 56 and 104 over 400 to 700, slopes, 576:   30.8 / 25.7 / 25.0  (41.0 / 37.3 / 40.6)
+//   four, 32 to 64 over 300 to 900, cap, 960:       34.6 / 28.8 / 26.7  (46.7 / 43.1 / 42.0)
 template <int D, int G, bool RULED = false>
 arb_status launch_one(Ctx *ctx, const F32ArgsOf<RULED> &a, cudaStream_t stream) {
     long long keys = a.max_pages * (long long)kPage;

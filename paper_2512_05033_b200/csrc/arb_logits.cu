@@ -12,7 +12,7 @@
 // best) go to the workspace; the CTA of a row that arrives last at the row's counter puts them together, run by run in order.
 //
 // What bounds it is instruction issue and the chain of steps before a window's stream.  64 rows of 128001 bf16 logits (49 MB; a
-// plain bf16 -> fp32 copy of them takes 24 us): 15 us without options, 26 with a history of up to 4096 tokens, 18 with 64 biases, 32 with
+// plain bf16 -> fp32 copy of them takes 24 us): 15 us without options, 26 with a history of up to 4096 tokens, 18 with 64 biases, 34 with
 // a history, biases, mask, temperature and noise (84 MB).  Special tokens found piece by piece, in a list in order of arrival and a counter
 // per token, 47 us; windows of 4 pieces instead of 8 39; a count and a bias looked up for every token 53; the special tokens in a kernel of
 // their own 61; a CTA per piece instead of a run of pieces 19 us without and 56 with everything (every CTA's reduction, fence and arrival

@@ -607,9 +607,9 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // alone are a kernel without the cap's code: prompts of documents 274 -> 231 us.
 // The bias.  -slope |pos - j|; keys of a tile that lies at or before the row's own key are at distance pos - key0 - k.
 constexpr float kCapPoly = 0.8f;
+constexpr double kCapFit[4] = {-0.33327582478523254, 0.13243256509304047, -0.049447160214185715, 0.012286622077226639};   // of P, in x^2
 // Caps up to this (1024, in log2 units) may take the form out of exponential and reciprocal, whose error of 2^-22 of the cap is then
-// a sixteenth of a weight's rounding to bf16; larger ones, and those the folded coefficients do not reach, take tanh_any, which keeps its relative
-// error down to 0.
+// a sixteenth of a weight's rounding to bf16; larger ones take tanh_any, which keeps its relative error down to 0.
 constexpr float kCapExpLog2 = 1024.f * 1.4426950408889634f;
 // The check needs a row's largest |s|.  While that is at most this (log2 units), it stands in for the row's maximum: any bound
 // serves a softmax whose weights keep their relative precision, and these lie above 2^-48.  One pass over the scores less.
@@ -626,6 +626,16 @@ __device__ __forceinline__ uint64_t capped2(const RuledArgs &a, uint64_t r, uint
     return fma_f32x2(r, fma_f32x2(p, w, scale2), add2);
 }
 
+// The same out of x = r to_cap, for caps so far from the scale that folded coefficients leave the normal numbers: eight operations.
+__device__ __forceinline__ uint64_t capped2_far(uint64_t r, uint64_t scale2, uint64_t to_cap2) {
+    const uint64_t x = mul_f32x2(r, to_cap2), s = mul_f32x2(r, scale2), w = mul_f32x2(x, x);
+    constexpr float c0 = (float)kCapFit[0], c1 = (float)kCapFit[1], c2 = (float)kCapFit[2], c3 = (float)kCapFit[3];
+    uint64_t p = fma_f32x2(both(c3), w, both(c2));
+    p = fma_f32x2(p, w, both(c1));
+    p = fma_f32x2(p, w, both(c0));
+    return fma_f32x2(s, mul_f32x2(p, w), s);
+}
+
 __device__ __forceinline__ uint64_t capped2(const MmaArgs &, uint64_t, uint64_t, uint64_t) { return 0; }   // (never called)
 
 template <bool BIAS>
@@ -640,26 +650,32 @@ __device__ __forceinline__ void apply_rules(const RuledArgs &a, uint32_t (&v)[kB
                 mx4[u] = max3(mx4[u], fabsf(__uint_as_float(v[k + 2 * u])), fabsf(__uint_as_float(v[k + 2 * u + 1])));
         }
         const float big = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * a.rules.to_cap;
-        const bool reach = !a.cap_plain || __any_sync(0xffffffffu, big > kCapPoly);
-        if (reach && a.rules.cap_log2 <= kCapExpLog2) {
+        const bool reach = __any_sync(0xffffffffu, big > kCapPoly);
+        if (!reach) {
+            const uint64_t scale2 = both(a.scale_log2), to_cap2 = both(a.rules.to_cap);
+            auto all = [&](auto plain_c) {
+#pragma unroll
+                for (int k = 0; k < kBN; k += 2) {
+                    const uint64_t r = pack_f32x2(__uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                    float lo, hi;
+                    if constexpr (decltype(plain_c)::value) unpack_f32x2(capped2(a, r, scale2, 0ull), lo, hi);
+                    else unpack_f32x2(capped2_far(r, scale2, to_cap2), lo, hi);
+                    v[k] = __float_as_uint(lo);
+                    v[k + 1] = __float_as_uint(hi);
+                }
+            };
+            if (a.cap_plain) all(std::true_type());
+            else all(std::false_type());
+        } else if (a.rules.cap_log2 <= kCapExpLog2) {
             // tanh(x) = 1 - 2 / (1 + e^(2 x)): off by 2^-22 or so absolute, the score by as much of the cap
             const float to_exp = a.rules.to_cap * 2.8853900817779268f;
 #pragma unroll
             for (int k = 0; k < kBN; ++k)
                 v[k] = __float_as_uint(a.rules.cap_log2 - __fdividef(2.0f * a.rules.cap_log2, 1.0f + fast_exp2(__uint_as_float(v[k]) * to_exp)));
-        } else if (reach) {
+        } else {
             // of a larger cap that is too much for the rows that do not reach it: their scores are small differences of it
 #pragma unroll
             for (int k = 0; k < kBN; ++k) v[k] = __float_as_uint(a.rules.cap_log2 * tanh_any(__uint_as_float(v[k]) * a.rules.to_cap));
-        } else {
-            const uint64_t scale2 = both(a.scale_log2);
-#pragma unroll
-            for (int k = 0; k < kBN; k += 2) {
-                float lo, hi;
-                unpack_f32x2(capped2(a, pack_f32x2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), scale2, 0ull), lo, hi);
-                v[k] = __float_as_uint(lo);
-                v[k + 1] = __float_as_uint(hi);
-            }
         }
     }
     if (BIAS && a.rules.slopes) {
@@ -1630,15 +1646,14 @@ inline void fill_args(MmaArgs &a, Ctx *ctx, const arb_attn_params &p, const void
 
 // The coefficients of capped2, from those of P(x^2).
 inline void fill_cap(RuledArgs &a) {
-    static const double fit[4] = {-0.33327582478523254, 0.13243256509304047, -0.049447160214185715, 0.012286622077226639};
     const double to_cap = a.rules.to_cap;
     double power = a.scale_log2;   // scale log2 e r times (to_cap r)^(2 i + 2)
     a.cap_plain = to_cap > 1e-4 && to_cap < 1e2;
     for (int i = 0; i < 4; ++i) {
         power *= to_cap * to_cap;
-        const double c = fabs(fit[i] * power);
+        const double c = fabs(kCapFit[i] * power);
         if (!(c > 1.2e-38 && c < 1e38)) a.cap_plain = 0;   // (of an unusual softmax scale)
-        a.cap_fit[i] = make_float2((float)(fit[i] * power), (float)(fit[i] * power));
+        a.cap_fit[i] = make_float2((float)(kCapFit[i] * power), (float)(kCapFit[i] * power));
     }
 }
 

@@ -601,7 +601,7 @@ __device__ __forceinline__ bool get_item(int item, int total, const Plan &pl, co
 // the weights (see `weights`): tanh is monotonic, so the maximum is taken of the raw products.  The others, which have hidden
 // keys or a bias to take in between, get it here.  Step-scoring batch (32 steps, 28 / 4 heads, cap 30): polynomial of degree 5 in a
 // pass of its own 560 us, taken on the way to the weights with the scale folded in 480, with 208 registers a softmax thread
-// (see setmaxnreg below; 168 spill) 470, with six operations and the bound below 455; arb_attn's kernel 285.  No pipe
+// (see setmaxnreg below; 168 spill) 470, with six operations and the bound below 441 to 455 by box; arb_attn's kernel 285.  No pipe
 // is the bound of that (the busiest is at 41 %); a tile's straight way of some 900 instructions outgrows the first instruction cache, and
 // waiting for instructions is the first stall.  Strict alternation of the polynomial and the exponentials took as long.  So ranges of keys
 // alone are a kernel without the cap's code: prompts of documents 274 -> 231 us.

@@ -188,3 +188,16 @@ def test_chunks_with_every_rule_off_are_the_plain_attentions(dtype, hq, hkv, D):
     assert bool((err <= bar).all())
     if D == 64:
         assert bool((err <= torch.finfo(dtype).eps / 2 * ref.abs() + (1e-5 if dtype == F32 else 1e-3)).all())
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 64)])
+@pytest.mark.parametrize("B", [33, 70, 300, 1024])
+def test_large_batches(dtype, D, B):
+    """More sequences than a warp plans for, up to the most a call takes: tokens, short steps and idle slots, whatever the window cuts off."""
+    r = np.random.RandomState(B)
+    lens = [int(v) for v in r.randint(1, 130, B)]
+    tokens = [int(v) for v in r.randint(0, 2, B)]
+    check(Inputs(32, dtype, 4, 2, D, lens, tokens[:-1] + [1], window=37, slopes=True))
+    new = [min(L, int(v)) for L, v in zip(lens, r.choice([0, 1, 2, 7], B))]
+    check(Inputs(33, dtype, 4, 2, D, lens, new[:-1] + [1], window=20, cap=8.0))
+    check(Inputs(34, dtype, 4, 2, D, lens, new[:-1] + [1], first=[int(v) for v in r.randint(0, 140, sum(new[:-1]) + 1)]))
